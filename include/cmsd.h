@@ -451,6 +451,110 @@ cmsd_status cmsd_draft_sample(const void* logits, int32_t dtype, int64_t n_rows,
  * (256 16-byte vectors) per row; 0 for n_rows <= 0 or an invalid vocab. */
 size_t cmsd_draft_sample_workspace_bytes(int64_t n_rows, int64_t vocab);
 
+/*
+ * The vocabulary projection ("head") around the logit pass: the product that makes logit
+ * rows, in 8-bit integers, and the loss that a drafter's head (or its trunk) is fitted with.
+ *
+ * cmsd_quantize_rows - rows to 8-bit codes with one scale each: scale = max|x| / 127 in
+ * single precision, code = the whole number next to x / scale, ties to even.  Quantises
+ * the head's weight once (a row per vocabulary entry) and the hidden rows per call.
+ *
+ *   rows        device, n_rows rows of `width` values, row r at element r*row_stride;
+ *               dtype CMSD_F32 or CMSD_BF16.  Any finite values; a row of zeros has
+ *               scale 0 and codes 0, and so has a row whose largest magnitude / 127
+ *               rounds to zero; a row that holds a NaN or an infinity has a NaN scale and
+ *               codes 0, so the logits made of it are NaN.
+ *   n_rows      >= 0 (0: nothing is enqueued), < 2^31.
+ *   width       >= 1, < 2^17; row_stride, code_stride >= width, < 2^40.
+ *   codes       device, n_rows rows of int8 at stride code_stride (output); what lies
+ *               between the rows is left alone.
+ *   scales      device, n_rows floats (output).
+ * Errors: CMSD_ERR_ARG, CMSD_ERR_DTYPE, CMSD_ERR_LAUNCH.
+ */
+cmsd_status cmsd_quantize_rows(const void* rows, int32_t dtype, int64_t n_rows, int64_t width, int64_t row_stride,
+                               int8_t* codes, int64_t code_stride, float* scales, void* stream);
+
+/*
+ * cmsd_head_logits - logit rows from quantised hidden rows and a quantised weight:
+ *   logits[n][v] = scale * hidden_scales[n] * weight_scales[v] * sum_k hidden[n][k] weight[v][k].
+ * The sum is formed in 32-bit integers and is exact (any codes, -128 among them); the
+ * scales are applied in single precision, and the result is rounded once to dtype.
+ *
+ *   hidden, weight  device, n_rows and vocab rows of `width` int8 codes.
+ *   hidden_scales   device, n_rows floats; weight_scales: device, vocab floats.
+ *   scale           finite: the model's own factor on its logits (1 for none).
+ *   n_rows          >= 0 (0: nothing is enqueued), < 2^24.
+ *   vocab in [2, 2^31), width in [1, 2^17); strides >= their rows' length, < 2^40.
+ *   logits          device, n_rows rows at stride logit_stride >= vocab (output), dtype
+ *                   CMSD_F32 or CMSD_BF16: rows as the other calls read them.  What lies
+ *                   between the rows is left alone.
+ * Any alignment of the codes and strides is right; rows that start at multiples of 16
+ * bytes (with a width that is one too) are read fastest.
+ * Errors: CMSD_ERR_ARG (a launch of 2^32 work-items or more among them), CMSD_ERR_DTYPE,
+ *         CMSD_ERR_LAUNCH.
+ */
+cmsd_status cmsd_head_logits(const int8_t* hidden, int64_t hidden_stride, const float* hidden_scales,
+                             const int8_t* weight, int64_t weight_stride, const float* weight_scales, float scale,
+                             int64_t n_rows, int64_t vocab, int64_t width, void* logits, int32_t dtype,
+                             int64_t logit_stride, void* stream);
+
+/*
+ * cmsd_head_loss - softmax cross entropy of hidden rows against token ids over the whole
+ * vocabulary, with z = scale * hidden . weight^T formed tile by tile and never stored:
+ *   lse[n] = ln sum_v exp z[n][v],  loss[n] = lse[n] - z[n][labels[n]].
+ *
+ *   hidden      device, n_rows rows of `width` values; weight: device, vocab rows.  Both of
+ *               dtype CMSD_F32 or CMSD_BF16; sums are held in single precision.
+ *   labels      device, n_rows int32.  A negative label has no loss (loss 0, lse as ever);
+ *               a label >= vocab is an error that the row reports: its loss is NaN.
+ *   scale       finite.
+ *   n_rows >= 0 (0: nothing is enqueued), < 2^24; vocab in [2, 2^31), width in [1, 2^17).
+ *   loss, lse   device, n_rows floats each (outputs).  Reductions over rows are the
+ *               caller's: grad_loss below carries their weights back.
+ *   workspace   device scratch of cmsd_head_loss_workspace_bytes(n_rows, vocab) bytes,
+ *               8-byte aligned, no initialisation needed.  Calls that share a workspace
+ *               must be ordered.
+ * Results are the same from run to run.  Errors: CMSD_ERR_ARG, CMSD_ERR_DTYPE,
+ * CMSD_ERR_LAUNCH.
+ */
+cmsd_status cmsd_head_loss(const void* hidden, int64_t hidden_stride, const void* weight, int64_t weight_stride,
+                           int32_t dtype, const int32_t* labels, float scale, int64_t n_rows, int64_t vocab,
+                           int64_t width, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/* Workspace of cmsd_head_loss; 0 for n_rows <= 0 or an invalid size. */
+size_t cmsd_head_loss_workspace_bytes(int64_t n_rows, int64_t vocab);
+
+/*
+ * cmsd_head_loss_grad - the gradients of sum_n grad_loss[n] * loss[n] by the hidden rows
+ * and by the weight, from the lse that cmsd_head_loss wrote:
+ *   d[n][v] = grad_loss[n] * scale * (exp(z[n][v] - lse[n]) - [v = labels[n]])
+ *   grad_hidden = d . weight,  grad_weight = d^T . hidden.
+ * The vocabulary is taken in pieces: a piece's logits are formed again and only its d is
+ * held, rounded to dtype as the products take it; the products are summed in single
+ * precision and rounded once.  Rows with a negative label, or one >= vocab, add nothing.
+ *
+ *   hidden .. width  as for cmsd_head_loss.  n_rows = 0 fills grad_weight with zeros.
+ *   lse, grad_loss   device, n_rows floats each.
+ *   grad_hidden      device, n_rows rows of dtype at stride grad_hidden_stride >= width
+ *                    (output), or NULL: not computed.
+ *   grad_weight      device, vocab rows of dtype at stride grad_weight_stride >= width
+ *                    (output), or NULL: not computed.  One of the two is given.  Neither
+ *                    may overlap hidden or weight.
+ *   workspace        device scratch of cmsd_head_loss_grad_workspace_bytes(n_rows, vocab,
+ *                    width, dtype) bytes, 16-byte aligned, no initialisation needed.
+ * Results are the same from run to run.  Errors: CMSD_ERR_ARG, CMSD_ERR_DTYPE,
+ * CMSD_ERR_LAUNCH.
+ */
+cmsd_status cmsd_head_loss_grad(const void* hidden, int64_t hidden_stride, const void* weight, int64_t weight_stride,
+                                int32_t dtype, const int32_t* labels, const float* lse, const float* grad_loss,
+                                float scale, int64_t n_rows, int64_t vocab, int64_t width, void* grad_hidden,
+                                int64_t grad_hidden_stride, void* grad_weight, int64_t grad_weight_stride,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace of cmsd_head_loss_grad; 0 for n_rows <= 0, an invalid size or dtype. */
+size_t cmsd_head_loss_grad_workspace_bytes(int64_t n_rows, int64_t vocab, int64_t width, int32_t dtype);
+
 /* Human-readable name of a status code (static string). */
 const char* cmsd_status_string(cmsd_status s);
 

@@ -14,6 +14,7 @@ import warnings
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "cmsd.hip")
+HEAD_SRC = os.path.join(PKG, "csrc", "head.hip")
 INC = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcmsd.so")
 
@@ -114,7 +115,7 @@ def build(verbose: bool = False) -> str:
     """Compile libcmsd.so, then the native test consumer, the probes and, where it can be,
     the native marshalling; returns the library's path.  Always recompiles."""
     tmp = LIB + ".tmp"
-    cmd = [hipcc(), f"--offload-arch={ARCH}", *FLAGS, "-I", INC, "-o", tmp, SRC]
+    cmd = [hipcc(), f"--offload-arch={ARCH}", *FLAGS, "-I", INC, "-o", tmp, SRC, HEAD_SRC]
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -88,6 +88,20 @@ def _load() -> C.CDLL:
     lib.cmsd_set_pass_decisions.restype = C.c_int
     lib.cmsd_logit_pass_fused_workspace_bytes.argtypes = [i32, i32, i64]
     lib.cmsd_logit_pass_fused_workspace_bytes.restype = C.c_size_t
+    f32, size = C.c_float, C.c_size_t
+    lib.cmsd_quantize_rows.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, vp]
+    lib.cmsd_quantize_rows.restype = C.c_int
+    lib.cmsd_head_logits.argtypes = [vp, i64, vp, vp, i64, vp, f32, i64, i64, i64, vp, i32, i64, vp]
+    lib.cmsd_head_logits.restype = C.c_int
+    lib.cmsd_head_loss.argtypes = [vp, i64, vp, i64, i32, vp, f32, i64, i64, i64, vp, vp, vp, size, vp]
+    lib.cmsd_head_loss.restype = C.c_int
+    lib.cmsd_head_loss_workspace_bytes.argtypes = [i64, i64]
+    lib.cmsd_head_loss_workspace_bytes.restype = size
+    lib.cmsd_head_loss_grad.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, f32, i64, i64, i64, vp, i64, vp, i64, vp,
+                                        size, vp]
+    lib.cmsd_head_loss_grad.restype = C.c_int
+    lib.cmsd_head_loss_grad_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.cmsd_head_loss_grad_workspace_bytes.restype = size
     lib.cmsd_status_string.argtypes = [C.c_int]
     lib.cmsd_status_string.restype = C.c_char_p
     lib.cmsd_version.argtypes = []
@@ -540,3 +554,163 @@ def cmsd_logit_pass_noalloc(draft_logits: torch.Tensor, target_logits: torch.Ten
         1 if adaptive else 0, _ptr(out["draft_stats"]), _ptr(out["draft_len"]), _ptr(out["target_stats"]),
         _ptr(out["n_accepted"]), _ptr(out["next_token"]), _stream(stream)))
     return out
+
+
+# ----------------------------------------------------------------------------- the vocabulary projection
+def _launch_on(fn: str, device: torch.device, stream, *args) -> None:
+    """The C call on ``stream`` (None: the current stream of the tensors' device), with
+    that device current."""
+    if torch.cuda.current_device() == device.index:
+        _check(fn, getattr(_lib, fn)(*args, _stream(stream)))
+        return
+    with torch.cuda.device(device):
+        _check(fn, getattr(_lib, fn)(*args, _stream(stream)))
+
+
+def _matrix(t: torch.Tensor, name: str, shape: tuple[int, int], dtype: torch.dtype, device: torch.device) -> int:
+    """Row stride of a caller's [rows, columns] buffer with unit inner stride whose rows do
+    not overlap."""
+    if t.dim() != 2 or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be of shape {shape}, not {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, not {t.device}")
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit inner stride")
+    if shape[0] > 1 and t.stride(0) < shape[1]:
+        raise ValueError(f"{name}'s rows overlap")
+    return max(t.stride(0), shape[1])
+
+
+def _width(t: torch.Tensor, name: str) -> tuple[int, int]:
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D [rows, width] tensor")
+    return t.shape[0], t.shape[1]
+
+
+def cmsd_quantize_rows(rows: torch.Tensor, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, *,
+                       stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Rows [n, width] (float32 or bfloat16) to int8 codes [n, width] and float32 scales
+    [n]: the largest magnitude of a row stands at 127.  For a head's weight (once) and for
+    hidden rows (per call of cmsd_head_logits)."""
+    n, W = _width(rows, "rows")
+    dev = rows.device
+    code = _dtype_code(rows)
+    st = _matrix(rows, "rows", (n, W), rows.dtype, dev)
+    if codes is None:
+        codes = torch.empty((n, W), dtype=torch.int8, device=dev)
+    if scales is None:
+        scales = torch.empty(n, dtype=torch.float32, device=dev)
+    cst = _matrix(codes, "codes", (n, W), torch.int8, dev)
+    _buf(scales, "scales", torch.float32, n, dev)
+    _on_device(rows, "rows")
+    _launch_on("cmsd_quantize_rows", dev, stream, _ptr(rows), code, n, W, st, _ptr(codes), cst, _ptr(scales))
+    return codes, scales
+
+
+def cmsd_head_logits(hidden: torch.Tensor, hidden_scales: torch.Tensor, weight: torch.Tensor,
+                     weight_scales: torch.Tensor, logits: torch.Tensor | None = None, *, scale: float = 1.0,
+                     dtype: torch.dtype = torch.bfloat16, stream=None) -> torch.Tensor:
+    """Logit rows [n, vocab] of quantised hidden rows [n, width] and a quantised weight
+    [vocab, width] (cmsd_quantize_rows), times ``scale``.  ``dtype`` (float32 or bfloat16)
+    is that of the rows made here where ``logits`` is not given."""
+    n, W = _width(hidden, "hidden")
+    V, _ = _width(weight, "weight")
+    dev = hidden.device
+    hst = _matrix(hidden, "hidden", (n, W), torch.int8, dev)
+    wst = _matrix(weight, "weight", (V, W), torch.int8, dev)
+    _buf(hidden_scales, "hidden_scales", torch.float32, n, dev)
+    _buf(weight_scales, "weight_scales", torch.float32, V, dev)
+    if logits is None:
+        logits = torch.empty((n, V), dtype=dtype, device=dev)
+    code = _dtype_code(logits)
+    lst = _matrix(logits, "logits", (n, V), logits.dtype, dev)
+    _on_device(hidden, "hidden")
+    _launch_on("cmsd_head_logits", dev, stream, _ptr(hidden), hst, _ptr(hidden_scales), _ptr(weight), wst,
+               _ptr(weight_scales), float(scale), n, V, W, _ptr(logits), code, lst)
+    return logits
+
+
+def cmsd_head_loss_workspace_bytes(n_rows: int, vocab: int) -> int:
+    return int(_lib.cmsd_head_loss_workspace_bytes(int(n_rows), int(vocab)))
+
+
+def cmsd_head_loss_grad_workspace_bytes(n_rows: int, vocab: int, width: int, dtype: torch.dtype) -> int:
+    return int(_lib.cmsd_head_loss_grad_workspace_bytes(int(n_rows), int(vocab), int(width),
+                                                        CMSD_F32 if dtype == torch.float32 else CMSD_BF16))
+
+
+def head_workspace(n_rows: int, vocab: int, width: int, dtype: torch.dtype, device, grad: bool = True) -> torch.Tensor:
+    """A device workspace for cmsd_head_loss and, with ``grad``, cmsd_head_loss_grad of
+    these sizes (allocate once, reuse across ordered calls)."""
+    n = cmsd_head_loss_workspace_bytes(n_rows, vocab)
+    if grad:
+        n = max(n, cmsd_head_loss_grad_workspace_bytes(n_rows, vocab, width, dtype))
+    return torch.empty((max(16, n) + 7) // 8, dtype=torch.float64, device=device)
+
+
+def _head(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor) -> tuple:
+    n, W = _width(hidden, "hidden")
+    V, _ = _width(weight, "weight")
+    dev = hidden.device
+    code = _dtype_code(hidden)
+    hst = _matrix(hidden, "hidden", (n, W), hidden.dtype, dev)
+    wst = _matrix(weight, "weight", (V, W), hidden.dtype, dev)
+    _buf(labels, "labels", torch.int32, n, dev)
+    return n, V, W, dev, code, hst, wst
+
+
+def _scratch(workspace: torch.Tensor | None, least: int, device: torch.device) -> torch.Tensor:
+    if workspace is None:
+        return torch.empty((max(16, least) + 7) // 8, dtype=torch.float64, device=device)
+    _buf(workspace, "workspace", workspace.dtype, 0, device)
+    if workspace.numel() * workspace.element_size() < least:
+        raise ValueError(f"workspace has {workspace.numel() * workspace.element_size()} bytes; {least} are needed")
+    return workspace
+
+
+def cmsd_head_loss(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, loss: torch.Tensor | None = None,
+                   lse: torch.Tensor | None = None, *, scale: float = 1.0, workspace: torch.Tensor | None = None,
+                   stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Softmax cross entropy of hidden rows [n, width] under a head's weight [vocab, width]
+    against labels [n] int32 (negative: no loss) -> (loss float32 [n], lse float32 [n]);
+    no logits are kept."""
+    n, V, W, dev, code, hst, wst = _head(hidden, weight, labels)
+    if loss is None:
+        loss = torch.empty(n, dtype=torch.float32, device=dev)
+    if lse is None:
+        lse = torch.empty(n, dtype=torch.float32, device=dev)
+    _buf(loss, "loss", torch.float32, n, dev)
+    _buf(lse, "lse", torch.float32, n, dev)
+    ws = _scratch(workspace, cmsd_head_loss_workspace_bytes(n, V), dev)
+    _on_device(hidden, "hidden")
+    _launch_on("cmsd_head_loss", dev, stream, _ptr(hidden), hst, _ptr(weight), wst, code, _ptr(labels), float(scale), n,
+               V, W, _ptr(loss), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size())
+    return loss, lse
+
+
+def cmsd_head_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor,
+                        grad_loss: torch.Tensor, grad_hidden: torch.Tensor | None = None,
+                        grad_weight: torch.Tensor | None = None, *, scale: float = 1.0,
+                        workspace: torch.Tensor | None = None,
+                        stream=None) -> tuple[torch.Tensor | None, torch.Tensor | None]:
+    """Gradients of sum_n grad_loss[n] * loss[n] by the hidden rows and the weight, into the
+    buffers given (of their shapes and type; None: not computed, at least one is given).
+    ``lse`` is cmsd_head_loss's."""
+    n, V, W, dev, code, hst, wst = _head(hidden, weight, labels)
+    _buf(lse, "lse", torch.float32, n, dev)
+    _buf(grad_loss, "grad_loss", torch.float32, n, dev)
+    if grad_hidden is None and grad_weight is None:
+        raise ValueError("one of grad_hidden and grad_weight is needed")
+    ghst = gwst = W
+    if grad_hidden is not None:
+        ghst = _matrix(grad_hidden, "grad_hidden", (n, W), hidden.dtype, dev)
+    if grad_weight is not None:
+        gwst = _matrix(grad_weight, "grad_weight", (V, W), hidden.dtype, dev)
+    ws = _scratch(workspace, cmsd_head_loss_grad_workspace_bytes(n, V, W, hidden.dtype), dev)
+    _on_device(hidden, "hidden")
+    _launch_on("cmsd_head_loss_grad", dev, stream, _ptr(hidden), hst, _ptr(weight), wst, code, _ptr(labels), _ptr(lse),
+               _ptr(grad_loss), float(scale), n, V, W, _ptr(grad_hidden), ghst, _ptr(grad_weight), gwst, _ptr(ws),
+               ws.numel() * ws.element_size())
+    return grad_hidden, grad_weight
