@@ -27,6 +27,7 @@ struct Bf16 {
 constexpr int kWave = 64;
 constexpr int kRowBytes = 128;  // of k that a tile holds per row: one cache line
 constexpr int kChunks = kRowBytes / 16;
+constexpr int kPad = 8;  // a logit gradient's rows are filled up to a multiple of so many
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -83,6 +84,7 @@ struct Side {
   const void* p;
   int64_t stride;
   int64_t rows;
+  int64_t k;  // of k that are there: a product's own k may be rounded up to whole chunks
 };
 
 // Where the tiles of a launch lie: tile (m, n) and part s of k.
@@ -138,7 +140,7 @@ struct Bring {
 #pragma unroll
           for (int j = 0; j < E; ++j) {
             x[j] = T{};
-            if (k + j < k_end) x[j] = p[(k + j) * s.stride + row];
+            if (k + j < k_end && k + j < s.k) x[j] = p[(k + j) * s.stride + row];
           }
           __builtin_memcpy(&v[i], x, 16);
         }
@@ -155,6 +157,27 @@ struct Bring {
     }
   }
 };
+
+// The tile of a workgroup.  Workgroups go round the eight dies by their number, and each die
+// has an L2 of its own: a die takes a run of tiles, and the run goes through blocks of
+// kBlockM tiles of m by all of n, m first, so that the 32 workgroups a die holds share
+// both operands' rows.
+constexpr int kDies = 8, kBlockM = 8;
+struct TileAt {
+  int m, n, part;
+};
+__device__ __forceinline__ TileAt tile_at(const Grid& g, uint32_t block) {
+  const uint32_t tiles = (uint32_t)g.tiles_m * (uint32_t)g.tiles_n, all = tiles * (uint32_t)g.parts;
+  const uint32_t die = block % kDies, of_die = block / kDies;
+  const uint32_t each = all / kDies, more = all % kDies;
+  const uint32_t at = die * each + (die < more ? die : more) + of_die;
+  const uint32_t part = at / tiles, i = at % tiles;
+  const uint32_t in_block = kBlockM * (uint32_t)g.tiles_n;
+  const uint32_t m0 = i / in_block * kBlockM;
+  const uint32_t high = (uint32_t)g.tiles_m - m0 < kBlockM ? (uint32_t)g.tiles_m - m0 : kBlockM;
+  const uint32_t j = i % in_block;
+  return TileAt{(int)(m0 + j % high), (int)(j / high), (int)part};
+}
 
 // ----------------------------------------------------------------------------- the product
 // A workgroup's tile of BM x BN, in WM x WN waves.
@@ -184,12 +207,9 @@ __global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g,
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave % TL::WM, wn = wave / TL::WM;
 
-  const uint32_t tiles = (uint32_t)g.tiles_m * (uint32_t)g.tiles_n;
-  const int part = blockIdx.x / tiles;
-  const uint32_t at = blockIdx.x % tiles;
-  const int tm = at / g.tiles_n, tn = at % g.tiles_n;
-  const int64_t m0 = (int64_t)tm * TL::BM, n0 = (int64_t)tn * TL::BN;
-  const int64_t k_begin = part * g.k_part;
+  const TileAt q = tile_at(g, blockIdx.x);
+  const int64_t m0 = (int64_t)q.m * TL::BM, n0 = (int64_t)q.n * TL::BN;
+  const int64_t k_begin = q.part * g.k_part;
   const int64_t k_end = k_begin + g.k_part < g.k ? k_begin + g.k_part : g.k;
 
   typename Mma<T>::Acc acc[TL::MI][TL::NI];
@@ -232,9 +252,209 @@ __global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g,
   w.n0 = n0 + wn * TL::NI * 16;
   w.wm = wm;
   w.lane = lane;
-  w.tile_m = tm;
-  w.part = part;
+  w.tile_m = q.m;
+  w.part = q.part;
   __syncthreads();  // the epilogue may take the LDS
+  e.template run<TL>(acc, w, a.rows, b.rows, lds, wn, t);
+}
+
+// ------------------------------------------------------- the product of aligned operands
+// The same product where both operands' rows start at multiples of 16 bytes and hold whole
+// 16-byte chunks: the tiles go from memory to LDS directly, a ring of STAGES of them deep,
+// and the workgroup waits for a tile's loads only when it takes the tile.
+//
+// Out of range: a side is read through a buffer descriptor that ends at its last row, and
+// everything past it comes as zeros.  Rows that the tile has too many give rows of the
+// output that are not stored.  For k past its end, a transposed side's rows end there; a
+// row-major side's chunks past it are asked for at an offset past every descriptor.
+//
+// LDS: a row-major side lies as in Bring.  A transposed side (k by k, ROWS values each) is
+// read through the transposing load (16-bit types): sixteen lanes take four k of sixteen
+// rows, 32 bytes of each of the four, and hold four k of a row each afterwards.  Pair of
+// chunks q of line k lies at position q ^ ((k & 3) | (k >> 1 & 4)): the eight lines that
+// thirty-two lanes take stand in banks of their own.  For 32-bit values a lane reads its
+// four k one by one, sixteen rows (four chunks) to a line: quad q at q ^ (k >> 2 & 3).  Lines
+// too short for either take as much of it as they have chunks.
+constexpr int kBufferFlags = 0x00020000;  // a raw buffer of 32-bit words
+constexpr uint32_t kNowhere = 0x80000000u;  // past every descriptor
+constexpr int64_t kMostRecords = 0x7fffffff;
+
+typedef __attribute__((address_space(3))) void* LdsPtr;
+
+template <typename T, int ROWS, int WAVES, Load LOAD>
+struct Stream {
+  static constexpr int E = 16 / sizeof(T);
+  static constexpr int BK = kRowBytes / sizeof(T);
+  static constexpr int BYTES = ROWS * kRowBytes;
+  static constexpr int N = BYTES / 1024 / WAVES;  // loads of a wave per tile
+  static_assert(N * WAVES * 1024 == BYTES, "whole loads per wave");
+  static constexpr int LINE = ROWS * (int)sizeof(T);  // bytes of one k of a transposed side
+
+  const char* base;
+  int64_t step;     // bytes from tile to tile
+  int64_t records;  // bytes from base to the side's end
+  uint32_t at[N];
+
+  static __device__ __forceinline__ int swizzle(int k) {
+    return (sizeof(T) == 2 ? ((k & 3) | ((k >> 1) & 4)) << 1 : ((k >> 2) & 3) << 2) & (LINE / 16 - 1);
+  }
+
+  __device__ __forceinline__ void init(const Side& s, int64_t row0, int64_t k0, int64_t k_end, int wave, int lane) {
+    const int64_t stride = s.stride * (int64_t)sizeof(T);
+    const char* p = static_cast<const char*>(s.p);
+    if (LOAD == Load::Rows) {
+      base = p + row0 * stride + k0 * (int64_t)sizeof(T);
+      step = kRowBytes;
+      const int64_t rows = s.rows - row0 < ROWS ? s.rows - row0 : ROWS;
+      records = (rows - 1) * stride + (k_end - k0) * (int64_t)sizeof(T);
+    } else {
+      k_end = k_end < s.k ? k_end : s.k;
+      base = p + k0 * stride + row0 * (int64_t)sizeof(T);
+      step = BK * stride;
+      // whole chunks: the caller's lines hold them, the workspace's are padded.  (The range
+      // check goes by 32-bit words, and the last line's last 16-bit value must not miss it.)
+      records = (k_end - k0 - 1) * stride + (s.rows - row0 + E - 1) / E * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int pos = (wave * N + i) * 64 + lane;  // 16-byte position in the tile
+      if (LOAD == Load::Rows) {
+        const int row = pos / kChunks, c = (pos % kChunks) ^ (row & 7);
+        at[i] = (uint32_t)(row * stride + c * 16);
+      } else {
+        const int k = pos / (LINE / 16), c = (pos % (LINE / 16)) ^ swizzle(k);
+        at[i] = (uint32_t)(k * stride + c * 16);
+      }
+    }
+  }
+  // The next tile, `left` elements of k from its start to the end.
+  __device__ __forceinline__ void load(char* lds, int64_t left, int wave, int lane) {
+    const int64_t n = records < kMostRecords ? records : kMostRecords;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(base), 0, __builtin_amdgcn_readfirstlane((int)n), kBufferFlags);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint32_t off = at[i];
+      if (LOAD == Load::Rows && left < BK) {
+        const int pos = (wave * N + i) * 64 + lane;
+        const int c = (pos % kChunks) ^ ((pos / kChunks) & 7);
+        if (c * E >= left) off = kNowhere;
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + (wave * N + i) * 1024), 16, off, 0, 0, 0);
+    }
+    base += step;
+    records -= step;
+  }
+  // Step s (of two, 64 bytes of k) of sixteen rows from row0 of the tile on.
+  static __device__ __forceinline__ u32x4 fragment(const char* lds, int row0, int s, int lane) {
+    const int g = lane >> 4, r = lane & 15;
+    if (LOAD == Load::Rows)
+      return *reinterpret_cast<const u32x4*>(lds + (row0 + r) * kRowBytes + (((s * 4 + g) ^ (lane & 7)) << 4));
+    if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((ext_vector_type(4))) short s16x4;
+      typedef __attribute__((address_space(3))) s16x4* P;
+      const int k = s * 32 + g * 8 + (r >> 2);
+      const int c = (row0 >> 3) + ((r & 3) >> 1);
+      const char* const a = lds + k * LINE + ((c ^ swizzle(k)) << 4) + (r & 1) * 8;
+      const char* const b = lds + (k + 4) * LINE + ((c ^ swizzle(k + 4)) << 4) + (r & 1) * 8;
+      const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)a), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)b);
+      const s16x4 v[2] = {x, y};
+      return __builtin_bit_cast(u32x4, v);
+    } else {
+      u32x4 v;
+      const int c = (row0 >> 2) + (r >> 2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = s * 16 + g * 4 + j;
+        v[j] = *reinterpret_cast<const uint32_t*>(lds + k * LINE + ((c ^ swizzle(k)) << 4) + (r & 3) * 4);
+      }
+      return v;
+    }
+  }
+};
+
+// Waits until at most N of the wave's loads are under way and all its LDS reads are done,
+// then for the other waves.
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <typename T, class TL, int STAGES, Load LA, Load LB, class Epilogue>
+__global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, Grid g, Epilogue e) {
+  typedef Stream<T, TL::BM, TL::WM * TL::WN, LA> SA;
+  typedef Stream<T, TL::BN, TL::WM * TL::WN, LB> SB;
+  constexpr int BK = kRowBytes / sizeof(T);
+  constexpr int STAGE = SA::BYTES + SB::BYTES;
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
+  const int t = threadIdx.x, lane = t & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wm = wave % TL::WM, wn = wave / TL::WM;
+
+  const TileAt q = tile_at(g, blockIdx.x);
+  const int64_t m0 = (int64_t)q.m * TL::BM, n0 = (int64_t)q.n * TL::BN;
+  const int64_t k_begin = q.part * g.k_part;
+  const int64_t k_end = k_begin + g.k_part < g.k ? k_begin + g.k_part : g.k;
+  const int tiles = (int)((k_end - k_begin + BK - 1) / BK);
+
+  typename Mma<T>::Acc acc[TL::MI][TL::NI];
+#pragma unroll
+  for (int i = 0; i < TL::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < TL::NI; ++j) acc[i][j] = typename Mma<T>::Acc{};
+
+  SA sa;
+  SB sb;
+  sa.init(a, m0, k_begin, k_end, wave, lane);
+  sb.init(b, n0, k_begin, k_end, wave, lane);
+  int64_t left = k_end - k_begin;
+  int into = 0, from = 0;  // stages, by their number
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) {
+    if (s < tiles) {
+      sa.load(lds + into * STAGE, left, wave, lane);
+      sb.load(lds + into * STAGE + SA::BYTES, left, wave, lane);
+      left -= BK;
+      into = into + 1 == STAGES ? 0 : into + 1;
+    }
+  }
+  for (int i = 0; i < tiles; ++i) {
+    // STAGES - 2 younger tiles may be under way; fewer are, near the end
+    if (STAGES > 2 && tiles - 1 - i >= STAGES - 2)
+      wait_and_meet<(STAGES - 2) * (SA::N + SB::N)>();
+    else
+      wait_and_meet<0>();
+    // every wave is done with the stage that the tile before lay in
+    if (left > 0) {
+      sa.load(lds + into * STAGE, left, wave, lane);
+      sb.load(lds + into * STAGE + SA::BYTES, left, wave, lane);
+      left -= BK;
+      into = into + 1 == STAGES ? 0 : into + 1;
+    }
+    const char* const la = lds + from * STAGE;
+    const char* const lb = la + SA::BYTES;
+    from = from + 1 == STAGES ? 0 : from + 1;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      u32x4 fa[TL::MI], fb[TL::NI];
+#pragma unroll
+      for (int i2 = 0; i2 < TL::MI; ++i2) fa[i2] = SA::fragment(la, wm * TL::MI * 16 + i2 * 16, s, lane);
+#pragma unroll
+      for (int j = 0; j < TL::NI; ++j) fb[j] = SB::fragment(lb, wn * TL::NI * 16 + j * 16, s, lane);
+#pragma unroll
+      for (int i2 = 0; i2 < TL::MI; ++i2)
+#pragma unroll
+        for (int j = 0; j < TL::NI; ++j) acc[i2][j] = Mma<T>::mma(fa[i2], fb[j], acc[i2][j]);
+    }
+  }
+  Place<TL> w;
+  w.m0 = m0 + wm * TL::MI * 16;
+  w.n0 = n0 + wn * TL::NI * 16;
+  w.wm = wm;
+  w.lane = lane;
+  w.tile_m = q.m;
+  w.part = q.part;
+  wait_and_meet<0>();  // the epilogue may take the LDS
   e.template run<TL>(acc, w, a.rows, b.rows, lds, wn, t);
 }
 
@@ -355,7 +575,8 @@ struct SoftmaxShares {
 };
 
 // The gradient by the logits, g * scale * (softmax - [v = label]), of a piece of the
-// vocabulary, rounded to the type of the products that take it.
+// vocabulary, rounded to the type of the products that take it.  Rows end in zeros up to a
+// whole chunk: k of the product that takes them along their length.
 template <typename T>
 struct LogitGradient {
   float scale;
@@ -368,6 +589,7 @@ struct LogitGradient {
 
   template <class TL, class Acc>
   __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, int64_t M, int64_t N, char*, int, int) const {
+    const int64_t filled = (M + kPad - 1) / kPad * kPad;
 #pragma unroll
     for (int j = 0; j < TL::NI; ++j) {
       const int64_t n = w.n(j);
@@ -378,14 +600,14 @@ struct LogitGradient {
 #pragma unroll
       for (int i = 0; i < TL::MI; ++i) {
         const int64_t m = w.m(i);
-        if (m >= M) continue;
+        if (m >= filled) continue;
         float x[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], mul, less));
-          x[r] = counts ? (p - (first + m + r == label ? 1.f : 0.f)) * g : 0.f;
+          x[r] = counts && m + r < M ? (p - (first + m + r == label ? 1.f : 0.f)) * g : 0.f;
         }
-        store4(out + n * stride + m, x, M - m);
+        store4(out + n * stride + m, x, filled - m);
       }
     }
   }
@@ -503,27 +725,79 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 bool launch_fits(int64_t groups, int threads) { return groups < ((int64_t)1 << 32) / threads; }
 
-typedef Tile<64, 64, 2, 2> SimpleTile;
+typedef Tile<64, 64, 2, 2> SimpleTile;  // operands of any alignment
 
 constexpr int64_t kMostRows = (int64_t)1 << 24;   // of hidden
 constexpr int64_t kMostWidth = (int64_t)1 << 17;  // an int32 sum of 2^17 - 1 products of codes holds
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 
-template <class TL>
-bool product_fits(int64_t rows_m, int64_t rows_n, int parts) {
-  return launch_fits(ceil_div(rows_m, TL::BM) * ceil_div(rows_n, TL::BN) * parts, TL::THREADS);
+// The tiles of aligned operands, by the output's extent: m (vocabulary or width) by n.
+enum class Shape { Simple, Large, Medium, Low, Few };
+struct LargeTile : Tile<256, 256, 2, 4> {
+  static constexpr int STAGES = 2;
+};
+struct MediumTile : Tile<128, 128, 2, 2> {
+  static constexpr int STAGES = 2;
+};
+struct LowTile : Tile<128, 64, 2, 2> {
+  static constexpr int STAGES = 3;
+};
+struct FewTile : Tile<128, 32, 4, 1> {
+  static constexpr int STAGES = 4;
+};
+Shape shape_of(int64_t m, int64_t n) {
+  if (n <= 32) return Shape::Few;
+  if (n <= 64) return Shape::Low;
+  if (ceil_div(m, 256) * ceil_div(n, 256) >= 192) return Shape::Large;
+  return Shape::Medium;
 }
+int tile_m(Shape s) { return s == Shape::Large ? 256 : s == Shape::Simple ? 64 : 128; }
+int tile_n(Shape s) {
+  return s == Shape::Large ? 256 : s == Shape::Medium ? 128 : s == Shape::Few ? 32 : 64;
+}
+int threads_of(Shape s) { return s == Shape::Large ? 512 : 256; }
+
+// Whether a side can be read directly: rows at multiples of 16 bytes, k (of a row-major
+// side; its length, of a transposed one) in whole chunks, a tile's offsets in 31 bits.
+template <typename T, Load LOAD>
+bool direct(const Side& s, int64_t k) {
+  constexpr int E = 16 / sizeof(T);
+  const int64_t along = LOAD == Load::Rows ? k : s.rows;
+  return ((uintptr_t)s.p & 15) == 0 && s.stride % E == 0 && (LOAD == Load::Columns || along % E == 0) &&
+         s.stride * (int64_t)sizeof(T) < (int64_t)1 << 22;
+}
+
 template <typename T, class TL, Load LA, Load LB, class Epilogue>
-void launch_product(const Side& a, const Side& b, int64_t k, int parts, const Epilogue& e, hipStream_t st) {
+void launch_direct(const Side& a, const Side& b, const Grid& g, unsigned groups, const Epilogue& e, hipStream_t st) {
+  hipLaunchKernelGGL((k_product_direct<T, TL, TL::STAGES, LA, LB, Epilogue>), dim3(groups), dim3(TL::THREADS), 0, st, a,
+                     b, g, e);
+}
+int64_t product_groups(Shape s, int64_t m, int64_t n, int parts) {
+  return ceil_div(m, tile_m(s)) * ceil_div(n, tile_n(s)) * parts;
+}
+bool product_fits(Shape s, int64_t m, int64_t n, int parts) {
+  return launch_fits(product_groups(s, m, n, parts), threads_of(s));
+}
+template <typename T, Load LA, Load LB, class Epilogue>
+void launch_product(Shape s, const Side& a, const Side& b, int64_t k, int parts, const Epilogue& e, hipStream_t st) {
   constexpr int BK = kRowBytes / sizeof(T);
   Grid g;
-  g.tiles_m = (int32_t)ceil_div(a.rows, TL::BM);
-  g.tiles_n = (int32_t)ceil_div(b.rows, TL::BN);
+  g.tiles_m = (int32_t)ceil_div(a.rows, tile_m(s));
+  g.tiles_n = (int32_t)ceil_div(b.rows, tile_n(s));
   g.k = k;
   g.k_part = round_up(ceil_div(k, parts), BK);
   g.parts = parts;
-  const int64_t groups = (int64_t)g.tiles_m * g.tiles_n * parts;
-  hipLaunchKernelGGL((k_product<T, TL, LA, LB, Epilogue>), dim3((unsigned)groups), dim3(TL::THREADS), 0, st, a, b, g, e);
+  const unsigned groups = (unsigned)product_groups(s, a.rows, b.rows, parts);
+  switch (s) {
+    case Shape::Simple:
+      hipLaunchKernelGGL((k_product<T, SimpleTile, LA, LB, Epilogue>), dim3(groups), dim3(SimpleTile::THREADS), 0, st, a,
+                         b, g, e);
+      break;
+    case Shape::Large: launch_direct<T, LargeTile, LA, LB>(a, b, g, groups, e, st); break;
+    case Shape::Medium: launch_direct<T, MediumTile, LA, LB>(a, b, g, groups, e, st); break;
+    case Shape::Low: launch_direct<T, LowTile, LA, LB>(a, b, g, groups, e, st); break;
+    case Shape::Few: launch_direct<T, FewTile, LA, LB>(a, b, g, groups, e, st); break;
+  }
 }
 
 bool sizes_ok(int64_t n_rows, int64_t vocab, int64_t width) {
@@ -538,13 +812,15 @@ bool finite(float x) { return x - x == 0.f; }
 // multiplied with the weight's rows (into the hidden rows' gradient) and with the hidden
 // rows (into the weight's).
 struct GradPlan {
-  int64_t piece;                   // vocabulary entries of a piece
+  int64_t piece, stride;           // vocabulary entries of a piece; a row of its gradients
+  Shape hidden_shape, weight_shape;
   int hidden_parts, weight_parts;  // parts of k of the two products
   size_t logits_at, hidden_at, weight_at, bytes;
 };
 constexpr int64_t kPieceBytes = (int64_t)1 << 28;  // of a piece's logit gradients
-int parts_for(int64_t tiles, int64_t k, int64_t least_k) {
-  int64_t parts = 1024 / (tiles < 1 ? 1 : tiles);
+int parts_for(Shape s, int64_t m, int64_t n, int64_t k, int64_t least_k) {
+  const int64_t tiles = product_groups(s, m, n, 1);
+  int64_t parts = 512 / tiles;
   const int64_t most = k / least_k;
   parts = parts < most ? parts : most;
   return (int)(parts < 1 ? 1 : (parts > 64 ? 64 : parts));
@@ -554,12 +830,14 @@ GradPlan grad_plan(int64_t n, int64_t vocab, int64_t width, int es) {
   p.piece = kPieceBytes / (n * es) / 256 * 256;
   if (p.piece < 256) p.piece = 256;
   if (p.piece > vocab) p.piece = vocab;
-  const int64_t stride = round_up(p.piece, 128);
-  p.hidden_parts = parts_for(ceil_div(width, 64) * ceil_div(n, 64), p.piece, 512);
-  p.weight_parts = parts_for(ceil_div(width, 64) * ceil_div(p.piece, 64), n, 512);
+  p.stride = round_up(p.piece, 128);
+  p.hidden_shape = shape_of(width, n);
+  p.weight_shape = shape_of(width, p.piece);
+  p.hidden_parts = parts_for(p.hidden_shape, width, n, p.piece, 512);
+  p.weight_parts = parts_for(p.weight_shape, width, p.piece, n, 512);
   size_t at = 0;
   p.logits_at = at;
-  at += (size_t)round_up(n * stride * es, 256);
+  at += (size_t)round_up(n * p.stride * es, 256);
   p.hidden_at = at;
   if (p.hidden_parts > 1 || p.piece < vocab) at += (size_t)round_up(p.hidden_parts * n * width * 4, 256);
   p.weight_at = at;
@@ -584,17 +862,18 @@ size_t loss_bytes(int64_t n, int64_t vocab) {
 
 template <typename T>
 cmsd_status enqueue_loss(const LossArgs& a, float* loss, float* lse, void* workspace, hipStream_t st) {
-  typedef SimpleTile TL;
+  const Side w{a.weight, a.weight_stride, a.vocab, a.width}, h{a.hidden, a.hidden_stride, a.n, a.width};
+  const bool fast = direct<T, Load::Rows>(w, a.width) && direct<T, Load::Rows>(h, a.width);
+  const Shape s = fast ? shape_of(a.vocab, a.n) : Shape::Simple;
+  if (!product_fits(s, a.vocab, a.n, 1)) return CMSD_ERR_ARG;
   SoftmaxShares e;
   e.scale = a.scale;
   e.labels = a.labels;
-  e.tiles_m = (int32_t)ceil_div(a.vocab, TL::BM);
+  e.tiles_m = (int32_t)ceil_div(a.vocab, tile_m(s));
   e.shares = static_cast<Share*>(workspace);
   e.at_label = reinterpret_cast<float*>(static_cast<char*>(workspace) +
                                         round_up(a.n * (int64_t)e.tiles_m * (int64_t)sizeof(Share), 256));
-  const Side w{a.weight, a.weight_stride, a.vocab}, h{a.hidden, a.hidden_stride, a.n};
-  if (!product_fits<TL>(a.vocab, a.n, 1)) return CMSD_ERR_ARG;
-  launch_product<T, TL, Load::Rows, Load::Rows>(w, h, a.width, 1, e, st);
+  launch_product<T, Load::Rows, Load::Rows>(s, w, h, a.width, 1, e, st);
   hipLaunchKernelGGL(k_loss, dim3((unsigned)ceil_div(a.n, 4)), dim3(256), 0, st, e.shares, e.tiles_m, e.at_label,
                      a.labels, a.n, a.vocab, loss, lse);
   return launched();
@@ -616,41 +895,46 @@ void sum_slabs(const float* slabs, int parts, int64_t slab, int64_t rows, int64_
 template <typename T>
 cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_loss, void* grad_hidden,
                          int64_t gh_stride, void* grad_weight, int64_t gw_stride, void* workspace, hipStream_t st) {
-  typedef SimpleTile TL;
   const GradPlan p = grad_plan(a.n, a.vocab, a.width, sizeof(T));
   char* const ws = static_cast<char*>(workspace);
   T* const dz = reinterpret_cast<T*>(ws + p.logits_at);
-  const int64_t dz_stride = round_up(p.piece, 128);
   float* const hs = reinterpret_cast<float*>(ws + p.hidden_at);
   float* const wsl = reinterpret_cast<float*>(ws + p.weight_at);
   const bool slabs = p.hidden_parts > 1 || p.piece < a.vocab;
-  const Side h{a.hidden, a.hidden_stride, a.n};
-  if (!product_fits<TL>(p.piece, a.n, 1) || (grad_hidden && !product_fits<TL>(a.width, a.n, p.hidden_parts)) ||
-      (grad_weight && !product_fits<TL>(a.width, p.piece, p.weight_parts)))
+  const Side h{a.hidden, a.hidden_stride, a.n, a.width}, ht{a.hidden, a.hidden_stride, a.width, a.n};
+  const Side w0{a.weight, a.weight_stride, a.vocab, a.width};
+  // the workspace's rows are aligned, and so are the operands' pieces where the operands are
+  const bool fast = direct<T, Load::Rows>(w0, a.width) && direct<T, Load::Rows>(h, a.width);
+  const Shape zs = fast ? shape_of(p.piece, a.n) : Shape::Simple;
+  const Shape hshape = fast ? p.hidden_shape : Shape::Simple, wshape = fast ? p.weight_shape : Shape::Simple;
+  if (!product_fits(zs, p.piece, a.n, 1) || (grad_hidden && !product_fits(hshape, a.width, a.n, p.hidden_parts)) ||
+      (grad_weight && !product_fits(wshape, a.width, p.piece, p.weight_parts)))
     return CMSD_ERR_ARG;
   for (int64_t v = 0; v < a.vocab; v += p.piece) {
     const int64_t m = a.vocab - v < p.piece ? a.vocab - v : p.piece;
-    const Side w{static_cast<const T*>(a.weight) + v * a.weight_stride, a.weight_stride, m};
-    LogitGradient<T> e{a.scale, a.labels, lse, grad_loss, v, a.vocab, dz, dz_stride};
-    launch_product<T, TL, Load::Rows, Load::Rows>(w, h, a.width, 1, e, st);
+    const T* const rows = static_cast<const T*>(a.weight) + v * a.weight_stride;
+    const Side w{rows, a.weight_stride, m, a.width};
+    LogitGradient<T> e{a.scale, a.labels, lse, grad_loss, v, a.vocab, dz, p.stride};
+    launch_product<T, Load::Rows, Load::Rows>(zs, w, h, a.width, 1, e, st);
     if (grad_hidden) {
-      const Side wt{w.p, w.stride, a.width}, d{dz, dz_stride, a.n};
+      const int64_t k = round_up(m, kPad);
+      const Side wt{rows, a.weight_stride, a.width, m}, d{dz, p.stride, a.n, k};
       if (slabs)
-        launch_product<T, TL, Load::Columns, Load::Rows>(wt, d, m, p.hidden_parts,
-                                                         Plain<float>{hs, a.width, a.n * a.width, v > 0}, st);
+        launch_product<T, Load::Columns, Load::Rows>(hshape, wt, d, k, p.hidden_parts,
+                                                     Plain<float>{hs, a.width, a.n * a.width, v > 0}, st);
       else
-        launch_product<T, TL, Load::Columns, Load::Rows>(
-            wt, d, m, 1, Plain<T>{static_cast<T*>(grad_hidden), gh_stride, 0, false}, st);
+        launch_product<T, Load::Columns, Load::Rows>(hshape, wt, d, k, 1,
+                                                     Plain<T>{static_cast<T*>(grad_hidden), gh_stride, 0, false}, st);
     }
     if (grad_weight) {
-      const Side ht{a.hidden, a.hidden_stride, a.width}, dt{dz, dz_stride, m};
+      const Side dt{dz, p.stride, m, a.n};
       T* const out = static_cast<T*>(grad_weight) + v * gw_stride;
       if (p.weight_parts > 1) {
-        launch_product<T, TL, Load::Columns, Load::Columns>(ht, dt, a.n, p.weight_parts,
-                                                            Plain<float>{wsl, a.width, m * a.width, false}, st);
+        launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, p.weight_parts,
+                                                        Plain<float>{wsl, a.width, m * a.width, false}, st);
         sum_slabs<T>(wsl, p.weight_parts, m * a.width, m, a.width, out, gw_stride, st);
       } else {
-        launch_product<T, TL, Load::Columns, Load::Columns>(ht, dt, a.n, 1, Plain<T>{out, gw_stride, 0, false}, st);
+        launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, 1, Plain<T>{out, gw_stride, 0, false}, st);
       }
     }
   }
@@ -720,16 +1004,18 @@ cmsd_status cmsd_head_logits(const int8_t* hidden, int64_t hidden_stride, const 
   if (!aligned(hidden_scales, 4) || !aligned(weight_scales, 4) || !aligned(logits, dtype == CMSD_F32 ? 4 : 2))
     return CMSD_ERR_ARG;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const Side w{weight, weight_stride, vocab}, h{hidden, hidden_stride, n_rows};
-  if (!product_fits<SimpleTile>(vocab, n_rows, 1)) return CMSD_ERR_ARG;
+  const Side w{weight, weight_stride, vocab, width}, h{hidden, hidden_stride, n_rows, width};
+  const bool fast = direct<int8_t, Load::Rows>(w, width) && direct<int8_t, Load::Rows>(h, width);
+  const Shape s = fast ? shape_of(vocab, n_rows) : Shape::Simple;
+  if (!product_fits(s, vocab, n_rows, 1)) return CMSD_ERR_ARG;
   if (dtype == CMSD_F32)
-    launch_product<int8_t, SimpleTile, Load::Rows, Load::Rows>(
-        w, h, width, 1, LogitRows<float>{hidden_scales, weight_scales, scale, static_cast<float*>(logits), logit_stride},
-        st);
+    launch_product<int8_t, Load::Rows, Load::Rows>(
+        s, w, h, width, 1,
+        LogitRows<float>{hidden_scales, weight_scales, scale, static_cast<float*>(logits), logit_stride}, st);
   else
-    launch_product<int8_t, SimpleTile, Load::Rows, Load::Rows>(
-        w, h, width, 1, LogitRows<Bf16>{hidden_scales, weight_scales, scale, static_cast<Bf16*>(logits), logit_stride},
-        st);
+    launch_product<int8_t, Load::Rows, Load::Rows>(
+        s, w, h, width, 1,
+        LogitRows<Bf16>{hidden_scales, weight_scales, scale, static_cast<Bf16*>(logits), logit_stride}, st);
   return launched();
 }
 

@@ -249,6 +249,54 @@ def test_grad_pieces_of_the_vocabulary(cm, dtype):
         assert far <= 1, float(far)
 
 
+def _on_gpu(h, wt, y, gl, scale, dtype):
+    """grad_bounds' references and bounds, and the loss's, formed on the GPU in float64."""
+    hd, wd = h.double(), wt.double()
+    keep = (y >= 0)[:, None]
+    z = scale * (hd @ wd.t().contiguous())
+    size = abs(scale) * (hd.abs() @ wd.abs().t().contiguous())
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    at_z = size * ((h.shape[1] + 4) * E) + z.abs() * E
+    at_lse = at_z.amax(1, keepdim=True) + 70 * E + 4 * E * lse.abs()
+    loss = torch.where(keep, lse - torch.gather(z, 1, y.long().clamp(min=0)[:, None]), 0.0)
+    p = torch.exp(z - lse)
+    g = gl.double()[:, None] * scale
+    at_p = p * (torch.expm1(at_z + at_lse + 4 * E * (z.abs() + lse.abs())) + 4 * E)
+    d = p.scatter_add(1, y.long().clamp(min=0)[:, None], torch.full_like(lse, -1.0)) * g * keep
+    at_d = (at_p * g.abs() * (1 + E) + d.abs() * (3 * E + UNIT[dtype])) * keep + 2.0 ** -133
+    ad = d.abs() + at_d
+    gh, gw = d @ wd, d.t().contiguous() @ hd
+    at_gh = at_d @ wd.abs() + (ad @ wd.abs()) * ((len(wt) + 70) * E) + gh.abs() * UNIT[dtype] * 1.01 + 2.0 ** -133
+    at_gw = at_d.t().contiguous() @ hd.abs() + (ad.t().contiguous() @ hd.abs()) * ((len(h) + 70) * E) \
+        + gw.abs() * UNIT[dtype] * 1.01 + 2.0 ** -133
+    return (loss[:, 0], (at_lse + at_z.amax(1, keepdim=True) + E * loss.abs())[:, 0]), (lse[:, 0], at_lse[:, 0]), \
+        (gh, at_gh), (gw, at_gw)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,v,w,pad", [(700, 17000, 64, 0), (3300, 600, 4096, 0), (300, 13000, 1024, 8),
+                                       (4100, 13001, 264, 0), (1024, 50257, 8, 0), (32, 50000, 136, 0),
+                                       (50, 30001, 520, 8)])
+def test_every_tile_of_the_products(cm, dtype, n, v, w, pad):
+    # extents that take the largest tiles in one product or another, and ragged ones in all
+    h, wt, y, _, _, _, gl = problem(n, n, v, w, dtype, pad)
+    gl = torch.from_numpy(gl).to(DEV)
+    loss, lse = cm.cmsd_head_loss(h, wt, y, scale=1.5)
+    gh, fh = padded(n, w, pad, dtype, -7.0)
+    gw, fw = padded(v, w, pad, dtype, -7.0)
+    cm.cmsd_head_loss_grad(h, wt, y, lse, gl, gh, gw, scale=1.5)
+    for got, (ref, bound), what in zip((loss, lse, gh, gw), _on_gpu(h, wt, y, gl, 1.5, dtype),
+                                       ("loss", "lse", "grad_hidden", "grad_weight")):
+        far = float(((got.double() - ref).abs() / bound).max())
+        assert far <= 1, (what, far)
+    assert gaps_left(fh, n, w, pad, -7.0) and gaps_left(fw, v, w, pad, -7.0)
+    c, s = cm.cmsd_quantize_rows(h)
+    wc, ws = cm.cmsd_quantize_rows(wt)
+    z = cm.cmsd_head_logits(c, s, wc, ws, dtype=dtype)
+    ref = (c.double() @ wc.double().t().contiguous()) * s[:, None].double() * ws.double()
+    assert bool(((z.double() - ref).abs() <= ref.abs() * (4 * 2.0 ** -24 + UNIT[dtype]) * 1.0001).all())
+
+
 def test_gradient_against_differences_of_the_loss(cm):
     n, v, w, scale = 6, 500, 64, 2.0
     h, wt, y, _, _, yy, gl = problem(9, n, v, w, F32, scale=scale)
