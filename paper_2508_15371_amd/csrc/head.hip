@@ -39,12 +39,9 @@ template <>
 __device__ __forceinline__ float from_float<float>(float x) {
   return x;
 }
-// To the nearest, ties to even; a NaN stays one.
 template <>
-__device__ __forceinline__ Bf16 from_float<Bf16>(float x) {
-  const uint32_t u = __float_as_uint(x);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return Bf16{(uint16_t)((u >> 16) | 0x40u)};
-  return Bf16{(uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16)};
+__device__ __forceinline__ Bf16 from_float<Bf16>(float x) {  // to the nearest, ties to even
+  return Bf16{__builtin_bit_cast(uint16_t, (__bf16)x)};
 }
 
 // ----------------------------------------------------------------------------- matrix cores
@@ -189,13 +186,32 @@ struct Tile {
   static constexpr int LDS = (BM + BN) * kRowBytes;
 };
 
+// Where a lane's values lie: value r of acc[i][j] is at m0 + m(i) + r, n0 + n(j).
 template <class TL>
-struct Place {  // where a lane's values of its wave's tile lie in the output
-  int64_t m0, n0;
-  int wm, lane, tile_m, part;
-  __device__ __forceinline__ int64_t m(int mi) const { return m0 + mi * 16 + (lane >> 4) * 4; }  // of four
-  __device__ __forceinline__ int64_t n(int ni) const { return n0 + ni * 16 + (lane & 15); }
+struct Place {
+  int64_t m0, n0;        // of the workgroup's tile
+  int left_m, left_n;    // what the output holds from there on, up to the tile's extent
+  int wm, wn, lane, t;
+  int tile_m, part;
+  __device__ __forceinline__ int m(int i) const { return wm * TL::MI * 16 + i * 16 + (lane >> 4) * 4; }
+  __device__ __forceinline__ int n(int j) const { return wn * TL::NI * 16 + j * 16 + (lane & 15); }
+  __device__ __forceinline__ bool whole() const { return left_m == TL::BM && left_n == TL::BN; }
 };
+template <class TL>
+__device__ __forceinline__ Place<TL> place_of(const TileAt& q, int64_t M, int64_t N, int wm, int wn, int lane, int t) {
+  Place<TL> w;
+  w.m0 = (int64_t)q.m * TL::BM;
+  w.n0 = (int64_t)q.n * TL::BN;
+  w.left_m = M - w.m0 < TL::BM ? (int)(M - w.m0) : TL::BM;
+  w.left_n = N - w.n0 < TL::BN ? (int)(N - w.n0) : TL::BN;
+  w.wm = wm;
+  w.wn = wn;
+  w.lane = lane;
+  w.t = t;
+  w.tile_m = q.m;
+  w.part = q.part;
+  return w;
+}
 
 template <typename T, class TL, Load LA, Load LB, class Epilogue>
 __global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g, Epilogue e) {
@@ -247,15 +263,8 @@ __global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g,
         for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[i], fb[j], acc[i][j]);
     }
   }
-  Place<TL> w;
-  w.m0 = m0 + wm * TL::MI * 16;
-  w.n0 = n0 + wn * TL::NI * 16;
-  w.wm = wm;
-  w.lane = lane;
-  w.tile_m = q.m;
-  w.part = q.part;
   __syncthreads();  // the epilogue may take the LDS
-  e.template run<TL>(acc, w, a.rows, b.rows, lds, wn, t);
+  e.template run<TL>(acc, place_of<TL>(q, a.rows, b.rows, wm, wn, lane, t), lds);
 }
 
 // ------------------------------------------------------- the product of aligned operands
@@ -281,11 +290,12 @@ constexpr int64_t kMostRecords = 0x7fffffff;
 
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
-template <typename T, int ROWS, int WAVES, Load LOAD>
+template <typename T, int ROWS, int WAVES, Load LOAD, int RB>
 struct Stream {
   static constexpr int E = 16 / sizeof(T);
-  static constexpr int BK = kRowBytes / sizeof(T);
-  static constexpr int BYTES = ROWS * kRowBytes;
+  static constexpr int BK = RB / sizeof(T);
+  static constexpr int CHUNKS = RB / 16;
+  static constexpr int BYTES = ROWS * RB;
   static constexpr int N = BYTES / 1024 / WAVES;  // loads of a wave per tile
   static_assert(N * WAVES * 1024 == BYTES, "whole loads per wave");
   static constexpr int LINE = ROWS * (int)sizeof(T);  // bytes of one k of a transposed side
@@ -295,6 +305,7 @@ struct Stream {
   int64_t records;  // bytes from base to the side's end
   uint32_t at[N];
 
+  static __device__ __forceinline__ int turn(int row) { return RB == 128 ? row & 7 : (row >> 1) & 3; }
   static __device__ __forceinline__ int swizzle(int k) {
     return (sizeof(T) == 2 ? ((k & 3) | ((k >> 1) & 4)) << 1 : ((k >> 2) & 3) << 2) & (LINE / 16 - 1);
   }
@@ -304,7 +315,7 @@ struct Stream {
     const char* p = static_cast<const char*>(s.p);
     if (LOAD == Load::Rows) {
       base = p + row0 * stride + k0 * (int64_t)sizeof(T);
-      step = kRowBytes;
+      step = RB;
       const int64_t rows = s.rows - row0 < ROWS ? s.rows - row0 : ROWS;
       records = (rows - 1) * stride + (k_end - k0) * (int64_t)sizeof(T);
     } else {
@@ -319,7 +330,7 @@ struct Stream {
     for (int i = 0; i < N; ++i) {
       const int pos = (wave * N + i) * 64 + lane;  // 16-byte position in the tile
       if (LOAD == Load::Rows) {
-        const int row = pos / kChunks, c = (pos % kChunks) ^ (row & 7);
+        const int row = pos / CHUNKS, c = (pos % CHUNKS) ^ turn(row);
         at[i] = (uint32_t)(row * stride + c * 16);
       } else {
         const int k = pos / (LINE / 16), c = (pos % (LINE / 16)) ^ swizzle(k);
@@ -327,29 +338,29 @@ struct Stream {
       }
     }
   }
-  // The next tile, `left` elements of k from its start to the end.
-  __device__ __forceinline__ void load(char* lds, int64_t left, int wave, int lane) {
+  // The next tile, `left` elements of k from its start to the end (none: zeros come, and no
+  // memory is read).
+  __device__ __forceinline__ void load(char* lds, int left, int wave, int lane) {
     const int64_t n = records < kMostRecords ? records : kMostRecords;
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<char*>(base), 0, __builtin_amdgcn_readfirstlane((int)n), kBufferFlags);
+        const_cast<char*>(base), 0, __builtin_amdgcn_readfirstlane(left > 0 ? (int)n : 0), kBufferFlags);
+    // a lane's chunk of its rows is the same in all its loads: they are 1024 bytes apart
+    const bool past = LOAD == Load::Rows && ((lane % CHUNKS) ^ turn(lane / CHUNKS)) * E >= left;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      uint32_t off = at[i];
-      if (LOAD == Load::Rows && left < BK) {
-        const int pos = (wave * N + i) * 64 + lane;
-        const int c = (pos % kChunks) ^ ((pos / kChunks) & 7);
-        if (c * E >= left) off = kNowhere;
-      }
+      const uint32_t off = past ? kNowhere : at[i];
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + (wave * N + i) * 1024), 16, off, 0, 0, 0);
     }
     base += step;
     records -= step;
   }
-  // Step s (of two, 64 bytes of k) of sixteen rows from row0 of the tile on.
-  static __device__ __forceinline__ u32x4 fragment(const char* lds, int row0, int s, int lane) {
+  // Step s (64 bytes of k) of sixteen rows from row0 of the tile on.  The pointer is said to
+  // be the only way to what it reads: the compiler would have the transposing load wait for
+  // every load to LDS under way (those go to another tile; wait_and_meet waits for this one's).
+  static __device__ __forceinline__ u32x4 fragment(const char* __restrict lds, int row0, int s, int lane) {
     const int g = lane >> 4, r = lane & 15;
     if (LOAD == Load::Rows)
-      return *reinterpret_cast<const u32x4*>(lds + (row0 + r) * kRowBytes + (((s * 4 + g) ^ (lane & 7)) << 4));
+      return *reinterpret_cast<const u32x4*>(lds + (row0 + r) * RB + (((s * 4 + g) ^ turn(r)) << 4));
     if constexpr (sizeof(T) == 2) {
       typedef __attribute__((ext_vector_type(4))) short s16x4;
       typedef __attribute__((address_space(3))) s16x4* P;
@@ -377,14 +388,40 @@ struct Stream {
 // then for the other waves.
 template <int N>
 __device__ __forceinline__ void wait_and_meet() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | (N >> 4) << 14);  // vmcnt N, lgkmcnt 0
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
-template <typename T, class TL, int STAGES, Load LA, Load LB, class Epilogue>
+// The order of a step's instructions: LDS reads (their values are the next step's), then
+// LOADS loads of a further tile, among the products.  A wave issues in order, and a load
+// or read that finds its pipeline full holds up the products behind it.
+template <class TL, typename T, Load LA, Load LB, int LOADS>
+__device__ __forceinline__ void interleave() {
+  constexpr int PER_A = LA == Load::Rows ? 1 : (sizeof(T) == 2 ? 2 : 4);
+  constexpr int PER_B = LB == Load::Rows ? 1 : (sizeof(T) == 2 ? 2 : 4);
+  constexpr int READS = TL::MI * PER_A + TL::NI * PER_B;
+  constexpr int MMAS = TL::MI * TL::NI * (sizeof(T) == 4 ? 4 : 1);
+  constexpr int EACH = MMAS / (READS + 2 * LOADS) > 0 ? MMAS / (READS + 2 * LOADS) : 1;
+#pragma unroll
+  for (int i = 0; i < READS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);    // an LDS read
+    __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);  // products
+  }
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);  // a load
+    __builtin_amdgcn_sched_group_barrier(0x008, 2 * EACH, 0);
+  }
+}
+
+template <typename T, class TL, int RB, int STAGES, Load LA, Load LB, class Epilogue>
 __global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, Grid g, Epilogue e) {
-  typedef Stream<T, TL::BM, TL::WM * TL::WN, LA> SA;
-  typedef Stream<T, TL::BN, TL::WM * TL::WN, LB> SB;
-  constexpr int BK = kRowBytes / sizeof(T);
+  typedef Stream<T, TL::BM, TL::WM * TL::WN, LA, RB> SA;
+  typedef Stream<T, TL::BN, TL::WM * TL::WN, LB, RB> SB;
+  constexpr int BK = SA::BK;
   constexpr int STAGE = SA::BYTES + SB::BYTES;
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
   const int t = threadIdx.x, lane = t & 63;
@@ -407,72 +444,117 @@ __global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, 
   SB sb;
   sa.init(a, m0, k_begin, k_end, wave, lane);
   sb.init(b, n0, k_begin, k_end, wave, lane);
-  int64_t left = k_end - k_begin;
-  int into = 0, from = 0;  // stages, by their number
+  int left = (int)(k_end - k_begin);
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s) {
-    if (s < tiles) {
-      sa.load(lds + into * STAGE, left, wave, lane);
-      sb.load(lds + into * STAGE + SA::BYTES, left, wave, lane);
-      left -= BK;
-      into = into + 1 == STAGES ? 0 : into + 1;
+  for (int s = 0; s < STAGES; ++s) {
+    sa.load(lds + s * STAGE, left, wave, lane);
+    sb.load(lds + s * STAGE + SA::BYTES, left, wave, lane);
+    left -= BK;
+  }
+  u32x4 fa[2][TL::MI], fb[2][TL::NI];
+  const auto read = [&](int to, int half, const char* tile) {
+#pragma unroll
+    for (int i = 0; i < TL::MI; ++i) fa[to][i] = SA::fragment(tile, wm * TL::MI * 16 + i * 16, half, lane);
+#pragma unroll
+    for (int j = 0; j < TL::NI; ++j) fb[to][j] = SB::fragment(tile + SA::BYTES, wn * TL::NI * 16 + j * 16, half, lane);
+  };
+  const auto multiply = [&](int from) {
+#pragma unroll
+    for (int i = 0; i < TL::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[from][i], fb[from][j], acc[i][j]);
+  };
+  // A step of 64 bytes of k is multiplied while the next is read.  Where the next lies in
+  // the next tile, the workgroup meets before it: that tile has arrived (the STAGES - 2
+  // behind it may be under way), and this one has been read by all, so its space takes a
+  // new one.
+  int stage = 0, done = 0;
+  const auto to_next_tile = [&](int from) {
+    char* const here = lds + stage * STAGE;
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    wait_and_meet<(STAGES - 2) * (SA::N + SB::N)>();
+    ++done;
+    sa.load(here, left, wave, lane);
+    sb.load(here + SA::BYTES, left, wave, lane);
+    left -= BK;
+    read(1 - from, 0, lds + stage * STAGE);  // of no use after the last tile
+    multiply(from);
+    interleave<TL, T, LA, LB, SA::N + SB::N>();
+  };
+  wait_and_meet<(STAGES - 1) * (SA::N + SB::N)>();
+  if (tiles > 0) read(0, 0, lds);
+  while (done < tiles) {
+    if constexpr (RB == 128) {
+      read(1, 1, lds + stage * STAGE);
+      multiply(0);
+      interleave<TL, T, LA, LB, 0>();
+      to_next_tile(1);
+    } else {
+      to_next_tile(0);
+      if (done == tiles) break;
+      to_next_tile(1);
     }
   }
-  for (int i = 0; i < tiles; ++i) {
-    // STAGES - 2 younger tiles may be under way; fewer are, near the end
-    if (STAGES > 2 && tiles - 1 - i >= STAGES - 2)
-      wait_and_meet<(STAGES - 2) * (SA::N + SB::N)>();
-    else
-      wait_and_meet<0>();
-    // every wave is done with the stage that the tile before lay in
-    if (left > 0) {
-      sa.load(lds + into * STAGE, left, wave, lane);
-      sb.load(lds + into * STAGE + SA::BYTES, left, wave, lane);
-      left -= BK;
-      into = into + 1 == STAGES ? 0 : into + 1;
-    }
-    const char* const la = lds + from * STAGE;
-    const char* const lb = la + SA::BYTES;
-    from = from + 1 == STAGES ? 0 : from + 1;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 fa[TL::MI], fb[TL::NI];
-#pragma unroll
-      for (int i2 = 0; i2 < TL::MI; ++i2) fa[i2] = SA::fragment(la, wm * TL::MI * 16 + i2 * 16, s, lane);
-#pragma unroll
-      for (int j = 0; j < TL::NI; ++j) fb[j] = SB::fragment(lb, wn * TL::NI * 16 + j * 16, s, lane);
-#pragma unroll
-      for (int i2 = 0; i2 < TL::MI; ++i2)
-#pragma unroll
-        for (int j = 0; j < TL::NI; ++j) acc[i2][j] = Mma<T>::mma(fa[i2], fb[j], acc[i2][j]);
-    }
-  }
-  Place<TL> w;
-  w.m0 = m0 + wm * TL::MI * 16;
-  w.n0 = n0 + wn * TL::NI * 16;
-  w.wm = wm;
-  w.lane = lane;
-  w.tile_m = q.m;
-  w.part = q.part;
   wait_and_meet<0>();  // the epilogue may take the LDS
-  e.template run<TL>(acc, w, a.rows, b.rows, lds, wn, t);
+  e.template run<TL>(acc, place_of<TL>(q, a.rows, b.rows, wm, wn, lane, t), lds);
 }
 
-// Four consecutive values of a row, as one vector where that is aligned and inside.
-template <typename T>
-__device__ __forceinline__ void store4(T* p, const float (&x)[4], int64_t left) {
-  struct alignas(4 * sizeof(T)) V {
-    T v[4];
-  };
-  if (left >= 4 && ((uintptr_t)p & (4 * sizeof(T) - 1)) == 0) {
-    V v;
+// Stores a wave's tile: value(i, j, r) of its lanes to row n0 + n(j), column m0 + m(i) + r of
+// `out`, as far as `left_m` columns and the tile's rows go.  Sixteen rows at a time pass
+// through the wave's own part of the LDS, so that a lane stores 16 bytes and a row's
+// lanes a contiguous run: stored from the accumulators, eight bytes of sixteen rows at a
+// time, a tile of 256 x 256 took a tenth of the time of its products over k = 4096.  (The
+// vectors may start at any element: the memory pipeline takes that.)  A wave's LDS
+// operations are done in their order.  add: to what is there.
+template <typename T, class TL, class F>
+__device__ __forceinline__ void store_rows(const Place<TL>& w, char* lds, T* out, int64_t stride, int left_m, bool add,
+                                           const F& value) {
+  constexpr int WIDTH = TL::MI * 16;                        // columns of the wave
+  constexpr int CHUNKS = WIDTH * (int)sizeof(T) / 16;       // of a row
+  constexpr int E = 16 / (int)sizeof(T);
+  constexpr int BYTES = 16 * WIDTH * (int)sizeof(T);        // of sixteen rows
+  static_assert(BYTES * TL::WM * TL::WN <= TL::LDS, "fits the tiles' space");
+  static_assert(BYTES % 1024 == 0 && (CHUNKS & (CHUNKS - 1)) == 0, "whole loads, a power of two of chunks");
+  char* const mine = lds + (w.wn * TL::WM + w.wm) * BYTES;
+  T* const o = out + w.n0 * stride + w.m0;
+  const int row = w.lane & 15, g = w.lane >> 4;
+  const bool whole = left_m >= TL::BM && w.left_n == TL::BN;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v.v[i] = from_float<T>(x[i]);
-    *reinterpret_cast<V*>(p) = v;
-  } else {
+  for (int j = 0; j < TL::NI; ++j) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < left) p[i] = from_float<T>(x[i]);
+    for (int i = 0; i < TL::MI; ++i) {
+      T v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = from_float<T>(value(i, j, r));
+      const int at = (i * 16 + g * 4) * (int)sizeof(T);  // chunk c of row r lies at c ^ r
+      __builtin_memcpy(__builtin_assume_aligned(
+                           mine + row * (CHUNKS * 16) + (((at >> 4) ^ (row & (CHUNKS - 1))) << 4) + (at & 15), 4 * sizeof(T)),
+                       v, sizeof v);
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < BYTES / 1024; ++k) {
+      const int at = k * 64 + w.lane, r = at / CHUNKS, c = (at % CHUNKS) ^ (r & (CHUNKS - 1));
+      T v[E];
+      __builtin_memcpy(v, __builtin_assume_aligned(mine + at * 16, 16), 16);
+      const int n = (w.wn * TL::NI + j) * 16 + r, m = w.wm * WIDTH + c * E;
+      T* const p = o + n * stride + m;
+      const int left = n < w.left_n ? left_m - m : 0;
+      if (whole || left >= E) {
+        if (add) {
+          T u[E];
+          __builtin_memcpy(u, p, 16);
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[e] = from_float<T>(to_float(v[e]) + to_float(u[e]));
+        }
+        __builtin_memcpy(p, v, 16);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (e < left) p[e] = add ? from_float<T>(to_float(v[e]) + to_float(p[e])) : v[e];
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -486,28 +568,24 @@ struct LogitRows {
   int64_t stride;
 
   template <class TL, class Acc>
-  __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, int64_t M, int64_t N, char*, int, int) const {
+  __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, char* lds) const {
+    float sw[TL::MI][4], sh[TL::NI];
 #pragma unroll
-    for (int i = 0; i < TL::MI; ++i) {
-      const int64_t m = w.m(i);
-      float sw[4];
+    for (int i = 0; i < TL::MI; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sw[r] = m + r < M ? weight_scales[m + r] : 0.f;
-#pragma unroll
-      for (int j = 0; j < TL::NI; ++j) {
-        const int64_t n = w.n(j);
-        if (n >= N || m >= M) continue;
-        const float sh = hidden_scales[n] * scale;
-        float x[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = (float)acc[i][j][r] * sh * sw[r];
-        store4(out + n * stride + m, x, M - m);
+      for (int r = 0; r < 4; ++r) {
+        const int m = w.m(i) + r;
+        sw[i][r] = weight_scales[w.m0 + (m < w.left_m ? m : 0)];
       }
-    }
+#pragma unroll
+    for (int j = 0; j < TL::NI; ++j) sh[j] = hidden_scales[w.n0 + (w.n(j) < w.left_n ? w.n(j) : 0)] * scale;
+    store_rows<T>(w, lds, out, stride, w.left_m, false,
+                  [&](int i, int j, int r) { return (float)acc[i][j][r] * sh[j] * sw[i][r]; });
   }
 };
 
-// A tile's share of a row's softmax: the largest logit and the sum of exponentials over it.
+// A tile's share of a row's softmax, in powers of two: the largest logit / ln 2 and the sum
+// of exponentials over it.
 struct Share {
   float top, sum;
 };
@@ -515,11 +593,19 @@ __device__ __forceinline__ Share join(Share x, Share y) {
   // the order of a pair changes nothing; an empty share (top = -inf, sum = 0) adds nothing
   const float top = fmaxf(x.top, y.top);
   if (top == -INFINITY) return Share{top, x.sum + y.sum};
-  return Share{top, x.sum * __builtin_amdgcn_exp2f((x.top - top) * kLog2e) +
-                        y.sum * __builtin_amdgcn_exp2f((y.top - top) * kLog2e)};
+  return Share{top, x.sum * __builtin_amdgcn_exp2f(x.top - top) + y.sum * __builtin_amdgcn_exp2f(y.top - top)};
 }
 
-// Shares of every row's softmax, and the label's logit.
+// Where entry v of the vocabulary lies from the lane's first column on, if its wave's tile
+// holds it, else -1.  (It is the lane's own if the place's low four bits are under four.)
+template <class TL>
+__device__ __forceinline__ int near(int64_t v, const Place<TL>& w) {
+  const int64_t at = v - w.m0 - w.m(0);
+  return at >= 0 && at < TL::MI * 16 && v - w.m0 < w.left_m ? (int)at : -1;
+}
+
+// Shares of every row's softmax, and the label's logit.  A NaN among the logits is not the
+// largest, but makes the sum one.
 struct SoftmaxShares {
   float scale;
   const int32_t* labels;
@@ -528,48 +614,57 @@ struct SoftmaxShares {
   float* at_label;  // [n]
 
   template <class TL, class Acc>
-  __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, int64_t M, int64_t N, char* lds, int wn,
-                                      int t) const {
+  __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, char* lds) const {
     Share* red = reinterpret_cast<Share*>(lds);  // [WM][BN]
     static_assert(TL::WM * TL::BN * (int)sizeof(Share) <= TL::LDS, "fits the tiles' space");
+    const float mul = scale * kLog2e;
+    const bool whole = w.left_m == TL::BM;
 #pragma unroll
     for (int j = 0; j < TL::NI; ++j) {
-      const int64_t n = w.n(j);
-      const int64_t label = n < N ? labels[n] : -1;
-      float top = -INFINITY;
-      bool bad = false;
+      const int at = w.n(j) < w.left_n ? near(labels[w.n0 + w.n(j)], w) : -1;
+      float top = -INFINITY, sum = 0.f;
+      if (whole) {
 #pragma unroll
-      for (int i = 0; i < TL::MI; ++i)
+        for (int i = 0; i < TL::MI; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t m = w.m(i) + r;
-          const float z = acc[i][j][r] * scale;
-          if (m < M) {
-            top = fmaxf(top, z);
-            bad |= z != z;
-            if (m == label) at_label[n] = z;
-          }
-        }
-      float sum = 0.f;
-      const float from = top == -INFINITY ? 0.f : top;
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r] * mul);
+        const float less = top == -INFINITY ? 0.f : -top;
 #pragma unroll
-      for (int i = 0; i < TL::MI; ++i)
+        for (int i = 0; i < TL::MI; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (w.m(i) + r < M) sum += __builtin_amdgcn_exp2f((acc[i][j][r] * scale - from) * kLog2e);
-      Share s{top, bad ? NAN : sum};
+          for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], mul, less));
+      } else {
+#pragma unroll
+        for (int i = 0; i < TL::MI; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (w.m(i) + r < w.left_m) top = fmaxf(top, acc[i][j][r] * mul);
+        const float less = top == -INFINITY ? 0.f : -top;
+#pragma unroll
+        for (int i = 0; i < TL::MI; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (w.m(i) + r < w.left_m) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], mul, less));
+      }
+      if (at >= 0) {
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < TL::MI; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) z = at == i * 16 + r ? acc[i][j][r] : z;
+        if ((at & 15) < 4) at_label[w.n0 + w.n(j)] = z * scale;
+      }
+      Share s{top, sum};
 #pragma unroll
       for (int d = 16; d < kWave; d *= 2) s = join(s, Share{__shfl_xor(s.top, d), __shfl_xor(s.sum, d)});
-      if (w.lane < 16) red[w.wm * TL::BN + wn * TL::NI * 16 + j * 16 + w.lane] = s;
+      if (w.lane < 16) red[w.wm * TL::BN + w.n(j)] = s;
     }
     __syncthreads();
-    for (int c = t; c < TL::BN; c += TL::THREADS) {
-      const int64_t n = w.n0 - wn * TL::NI * 16 + c;
-      if (n >= N) continue;
+    for (int c = w.t; c < w.left_n; c += TL::THREADS) {
       Share s = red[c];
 #pragma unroll
       for (int k = 1; k < TL::WM; ++k) s = join(s, red[k * TL::BN + c]);
-      shares[n * tiles_m + w.tile_m] = s;
+      shares[(w.n0 + c) * tiles_m + w.tile_m] = s;
     }
   }
 };
@@ -588,28 +683,30 @@ struct LogitGradient {
   int64_t stride;
 
   template <class TL, class Acc>
-  __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, int64_t M, int64_t N, char*, int, int) const {
-    const int64_t filled = (M + kPad - 1) / kPad * kPad;
+  __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, char* lds) const {
+    const float mul = scale * kLog2e;
+    float less[TL::NI], g[TL::NI];
+    int at[TL::NI];
+    bool counts[TL::NI];
 #pragma unroll
     for (int j = 0; j < TL::NI; ++j) {
-      const int64_t n = w.n(j);
-      if (n >= N) continue;
+      const int64_t n = w.n0 + (w.n(j) < w.left_n ? w.n(j) : 0);
       const int64_t label = labels[n];
-      const bool counts = label >= 0 && label < vocab;
-      const float g = grad_loss[n] * scale, less = -lse[n] * kLog2e, mul = scale * kLog2e;
-#pragma unroll
-      for (int i = 0; i < TL::MI; ++i) {
-        const int64_t m = w.m(i);
-        if (m >= filled) continue;
-        float x[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], mul, less));
-          x[r] = counts && m + r < M ? (p - (first + m + r == label ? 1.f : 0.f)) * g : 0.f;
-        }
-        store4(out + n * stride + m, x, filled - m);
-      }
+      counts[j] = label >= 0 && label < vocab;
+      g[j] = grad_loss[n] * scale;
+      less[j] = -lse[n] * kLog2e;
+      at[j] = near(label - first, w);
     }
+    const int filled = (w.left_m + kPad - 1) / kPad * kPad;
+    const auto value = [&](int i, int j, int r) {
+      const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], mul, less[j]));
+      return counts[j] ? (at[j] == i * 16 + r ? p - 1.f : p) * g[j] : 0.f;
+    };
+    if (w.left_m == TL::BM)
+      store_rows<T>(w, lds, out, stride, filled, false, value);
+    else
+      store_rows<T>(w, lds, out, stride, filled, false,
+                    [&](int i, int j, int r) { return w.m(i) + r < w.left_m ? value(i, j, r) : 0.f; });
   }
 };
 
@@ -622,24 +719,8 @@ struct Plain {
   bool add;
 
   template <class TL, class Acc>
-  __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, int64_t M, int64_t N, char*, int, int) const {
-    T* const o = out + w.part * slab;
-#pragma unroll
-    for (int j = 0; j < TL::NI; ++j) {
-      const int64_t n = w.n(j);
-#pragma unroll
-      for (int i = 0; i < TL::MI; ++i) {
-        const int64_t m = w.m(i);
-        if (n >= N || m >= M) continue;
-        float x[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[r] = acc[i][j][r];
-          if (add && m + r < M) x[r] += to_float(o[n * stride + m + r]);
-        }
-        store4(o + n * stride + m, x, M - m);
-      }
-    }
+  __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, char* lds) const {
+    store_rows<T>(w, lds, out + w.part * slab, stride, w.left_m, add, [&](int i, int j, int r) { return acc[i][j][r]; });
   }
 };
 
@@ -661,7 +742,7 @@ __global__ __launch_bounds__(256) void k_loss(const Share* shares, int32_t tiles
   for (int i = lane; i < tiles_m; i += kWave) s = join(s, shares[n * tiles_m + i]);
   s = wave_join(s);
   if (lane == 0) {
-    const float l = s.top + logf(s.sum);
+    const float l = (s.top + log2f(s.sum)) * kLn2;
     const int64_t label = labels[n];
     lse[n] = l;
     loss[n] = label < 0 ? 0.f : (label < vocab ? l - at_label[n] : NAN);
@@ -731,31 +812,25 @@ constexpr int64_t kMostRows = (int64_t)1 << 24;   // of hidden
 constexpr int64_t kMostWidth = (int64_t)1 << 17;  // an int32 sum of 2^17 - 1 products of codes holds
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 
-// The tiles of aligned operands, by the output's extent: m (vocabulary or width) by n.
+// The tiles of aligned operands, m (vocabulary or width) by n.
 enum class Shape { Simple, Large, Medium, Low, Few };
-struct LargeTile : Tile<256, 256, 2, 4> {
-  static constexpr int STAGES = 2;
+struct LargeTile : Tile<256, 256, 2, 4> {  // one workgroup per compute unit
+  static constexpr int RB = 128, STAGES = 2;
 };
-struct MediumTile : Tile<128, 128, 2, 2> {
-  static constexpr int STAGES = 2;
+struct MediumTile : Tile<128, 128, 2, 4> {  // two
+  static constexpr int RB = 128, STAGES = 2;
 };
 struct LowTile : Tile<128, 64, 2, 2> {
-  static constexpr int STAGES = 3;
+  static constexpr int RB = 128, STAGES = 3;
 };
 struct FewTile : Tile<128, 32, 4, 1> {
-  static constexpr int STAGES = 4;
+  static constexpr int RB = 128, STAGES = 4;
 };
-Shape shape_of(int64_t m, int64_t n) {
-  if (n <= 32) return Shape::Few;
-  if (n <= 64) return Shape::Low;
-  if (ceil_div(m, 256) * ceil_div(n, 256) >= 192) return Shape::Large;
-  return Shape::Medium;
-}
 int tile_m(Shape s) { return s == Shape::Large ? 256 : s == Shape::Simple ? 64 : 128; }
 int tile_n(Shape s) {
   return s == Shape::Large ? 256 : s == Shape::Medium ? 128 : s == Shape::Few ? 32 : 64;
 }
-int threads_of(Shape s) { return s == Shape::Large ? 512 : 256; }
+int threads_of(Shape s) { return s == Shape::Large || s == Shape::Medium ? 512 : 256; }
 
 // Whether a side can be read directly: rows at multiples of 16 bytes, k (of a row-major
 // side; its length, of a transposed one) in whole chunks, a tile's offsets in 31 bits.
@@ -769,18 +844,54 @@ bool direct(const Side& s, int64_t k) {
 
 template <typename T, class TL, Load LA, Load LB, class Epilogue>
 void launch_direct(const Side& a, const Side& b, const Grid& g, unsigned groups, const Epilogue& e, hipStream_t st) {
-  hipLaunchKernelGGL((k_product_direct<T, TL, TL::STAGES, LA, LB, Epilogue>), dim3(groups), dim3(TL::THREADS), 0, st, a,
+  hipLaunchKernelGGL((k_product_direct<T, TL, TL::RB, TL::STAGES, LA, LB, Epilogue>), dim3(groups), dim3(TL::THREADS), 0, st, a,
                      b, g, e);
 }
 int64_t product_groups(Shape s, int64_t m, int64_t n, int parts) {
   return ceil_div(m, tile_m(s)) * ceil_div(n, tile_n(s)) * parts;
+}
+// The shape of an m x n product over k, and the parts that k is cut into.
+struct Cut {
+  Shape shape;
+  int parts;
+};
+// Few rows (n) take tiles as low as they are: such a product reads its weight once and is
+// bound by that.  Else large or medium tiles and, where most_parts allows, parts of k, by
+// what they are expected to take: rounds of workgroups over the chip, each round its tiles
+// of 128 bytes of k and a start and an end worth some more, and the slabs of parts written
+// and read.  Measured on 256 compute units, us per tile of k and round: 16-bit and 8-bit
+// types large 1.45, medium 0.92 (two workgroups), 32-bit 7.2 and 3.6 (bound by the matrix
+// cores alike).  16384 x 8192 x 4096, bf16: large 0.77 ms, medium 0.94; 50257 x 1000 x 768
+// 96 and 90 us; 1024 x 4096 over k = 32000 in 1 and 4 parts: large 0.69 and 0.22 ms,
+// medium 0.41 and 0.28.
+Cut cut_of(int64_t m, int64_t n, int64_t k, int es, int most_parts) {
+  const int64_t tiles_k = ceil_div(k * es, kRowBytes);
+  if (n <= 64 && most_parts <= 1) return Cut{n <= 32 ? Shape::Few : Shape::Low, 1};
+  Cut best{Shape::Medium, 1};
+  double least = INFINITY;
+  for (const Shape s : {Shape::Large, Shape::Medium}) {
+    const bool large = s == Shape::Large;
+    const double unit = es == 4 ? (large ? 7.2 : 3.6) : (large ? 1.45 : 0.92);
+    const double more = es == 4 ? 1.0 : (large ? 5.0 : 2.0);
+    const int64_t tiles = product_groups(s, m, n, 1), slots = large ? 256 : 512;
+    for (int parts = 1; parts <= most_parts && (parts == 1 || tiles_k / parts >= 4); ++parts) {
+      const double slabs = parts > 1 ? 2.0 * parts * m * n * 4 / 4e6 : 0.0;
+      if (slabs > 250.0) break;
+      const double us = ceil_div(tiles * parts, slots) * (ceil_div(tiles_k, parts) + more) * unit + slabs;
+      if (us < least) {
+        least = us;
+        best = Cut{s, parts};
+      }
+    }
+  }
+  return best;
 }
 bool product_fits(Shape s, int64_t m, int64_t n, int parts) {
   return launch_fits(product_groups(s, m, n, parts), threads_of(s));
 }
 template <typename T, Load LA, Load LB, class Epilogue>
 void launch_product(Shape s, const Side& a, const Side& b, int64_t k, int parts, const Epilogue& e, hipStream_t st) {
-  constexpr int BK = kRowBytes / sizeof(T);
+  constexpr int BK = kRowBytes / sizeof(T);  // a multiple of every tile's k
   Grid g;
   g.tiles_m = (int32_t)ceil_div(a.rows, tile_m(s));
   g.tiles_n = (int32_t)ceil_div(b.rows, tile_n(s));
@@ -812,36 +923,26 @@ bool finite(float x) { return x - x == 0.f; }
 // multiplied with the weight's rows (into the hidden rows' gradient) and with the hidden
 // rows (into the weight's).
 struct GradPlan {
-  int64_t piece, stride;           // vocabulary entries of a piece; a row of its gradients
-  Shape hidden_shape, weight_shape;
-  int hidden_parts, weight_parts;  // parts of k of the two products
+  int64_t piece, stride;  // vocabulary entries of a piece; a row of its gradients
+  Cut hidden, weight;     // the two products that take them
   size_t logits_at, hidden_at, weight_at, bytes;
 };
 constexpr int64_t kPieceBytes = (int64_t)1 << 28;  // of a piece's logit gradients
-int parts_for(Shape s, int64_t m, int64_t n, int64_t k, int64_t least_k) {
-  const int64_t tiles = product_groups(s, m, n, 1);
-  int64_t parts = 512 / tiles;
-  const int64_t most = k / least_k;
-  parts = parts < most ? parts : most;
-  return (int)(parts < 1 ? 1 : (parts > 64 ? 64 : parts));
-}
 GradPlan grad_plan(int64_t n, int64_t vocab, int64_t width, int es) {
   GradPlan p;
   p.piece = kPieceBytes / (n * es) / 256 * 256;
   if (p.piece < 256) p.piece = 256;
   if (p.piece > vocab) p.piece = vocab;
   p.stride = round_up(p.piece, 128);
-  p.hidden_shape = shape_of(width, n);
-  p.weight_shape = shape_of(width, p.piece);
-  p.hidden_parts = parts_for(p.hidden_shape, width, n, p.piece, 512);
-  p.weight_parts = parts_for(p.weight_shape, width, p.piece, n, 512);
+  p.hidden = cut_of(width, n, p.piece, es, 64);
+  p.weight = cut_of(width, p.piece, n, es, 64);
   size_t at = 0;
   p.logits_at = at;
   at += (size_t)round_up(n * p.stride * es, 256);
   p.hidden_at = at;
-  if (p.hidden_parts > 1 || p.piece < vocab) at += (size_t)round_up(p.hidden_parts * n * width * 4, 256);
+  if (p.hidden.parts > 1 || p.piece < vocab) at += (size_t)round_up(p.hidden.parts * n * width * 4, 256);
   p.weight_at = at;
-  if (p.weight_parts > 1) at += (size_t)round_up(p.weight_parts * p.piece * width * 4, 256);
+  if (p.weight.parts > 1) at += (size_t)round_up(p.weight.parts * p.piece * width * 4, 256);
   p.bytes = at;
   return p;
 }
@@ -864,7 +965,7 @@ template <typename T>
 cmsd_status enqueue_loss(const LossArgs& a, float* loss, float* lse, void* workspace, hipStream_t st) {
   const Side w{a.weight, a.weight_stride, a.vocab, a.width}, h{a.hidden, a.hidden_stride, a.n, a.width};
   const bool fast = direct<T, Load::Rows>(w, a.width) && direct<T, Load::Rows>(h, a.width);
-  const Shape s = fast ? shape_of(a.vocab, a.n) : Shape::Simple;
+  const Shape s = fast ? cut_of(a.vocab, a.n, a.width, sizeof(T), 1).shape : Shape::Simple;
   if (!product_fits(s, a.vocab, a.n, 1)) return CMSD_ERR_ARG;
   SoftmaxShares e;
   e.scale = a.scale;
@@ -900,15 +1001,15 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
   T* const dz = reinterpret_cast<T*>(ws + p.logits_at);
   float* const hs = reinterpret_cast<float*>(ws + p.hidden_at);
   float* const wsl = reinterpret_cast<float*>(ws + p.weight_at);
-  const bool slabs = p.hidden_parts > 1 || p.piece < a.vocab;
+  const bool slabs = p.hidden.parts > 1 || p.piece < a.vocab;
   const Side h{a.hidden, a.hidden_stride, a.n, a.width}, ht{a.hidden, a.hidden_stride, a.width, a.n};
   const Side w0{a.weight, a.weight_stride, a.vocab, a.width};
   // the workspace's rows are aligned, and so are the operands' pieces where the operands are
   const bool fast = direct<T, Load::Rows>(w0, a.width) && direct<T, Load::Rows>(h, a.width);
-  const Shape zs = fast ? shape_of(p.piece, a.n) : Shape::Simple;
-  const Shape hshape = fast ? p.hidden_shape : Shape::Simple, wshape = fast ? p.weight_shape : Shape::Simple;
-  if (!product_fits(zs, p.piece, a.n, 1) || (grad_hidden && !product_fits(hshape, a.width, a.n, p.hidden_parts)) ||
-      (grad_weight && !product_fits(wshape, a.width, p.piece, p.weight_parts)))
+  const Shape zs = fast ? cut_of(p.piece, a.n, a.width, sizeof(T), 1).shape : Shape::Simple;
+  const Shape hshape = fast ? p.hidden.shape : Shape::Simple, wshape = fast ? p.weight.shape : Shape::Simple;
+  if (!product_fits(zs, p.piece, a.n, 1) || (grad_hidden && !product_fits(hshape, a.width, a.n, p.hidden.parts)) ||
+      (grad_weight && !product_fits(wshape, a.width, p.piece, p.weight.parts)))
     return CMSD_ERR_ARG;
   for (int64_t v = 0; v < a.vocab; v += p.piece) {
     const int64_t m = a.vocab - v < p.piece ? a.vocab - v : p.piece;
@@ -920,7 +1021,7 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
       const int64_t k = round_up(m, kPad);
       const Side wt{rows, a.weight_stride, a.width, m}, d{dz, p.stride, a.n, k};
       if (slabs)
-        launch_product<T, Load::Columns, Load::Rows>(hshape, wt, d, k, p.hidden_parts,
+        launch_product<T, Load::Columns, Load::Rows>(hshape, wt, d, k, p.hidden.parts,
                                                      Plain<float>{hs, a.width, a.n * a.width, v > 0}, st);
       else
         launch_product<T, Load::Columns, Load::Rows>(hshape, wt, d, k, 1,
@@ -929,17 +1030,17 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
     if (grad_weight) {
       const Side dt{dz, p.stride, m, a.n};
       T* const out = static_cast<T*>(grad_weight) + v * gw_stride;
-      if (p.weight_parts > 1) {
-        launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, p.weight_parts,
+      if (p.weight.parts > 1) {
+        launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, p.weight.parts,
                                                         Plain<float>{wsl, a.width, m * a.width, false}, st);
-        sum_slabs<T>(wsl, p.weight_parts, m * a.width, m, a.width, out, gw_stride, st);
+        sum_slabs<T>(wsl, p.weight.parts, m * a.width, m, a.width, out, gw_stride, st);
       } else {
         launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, 1, Plain<T>{out, gw_stride, 0, false}, st);
       }
     }
   }
   if (grad_hidden && slabs)
-    sum_slabs<T>(hs, p.hidden_parts, a.n * a.width, a.n, a.width, grad_hidden, gh_stride, st);
+    sum_slabs<T>(hs, p.hidden.parts, a.n * a.width, a.n, a.width, grad_hidden, gh_stride, st);
   return launched();
 }
 
@@ -1006,7 +1107,7 @@ cmsd_status cmsd_head_logits(const int8_t* hidden, int64_t hidden_stride, const 
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Side w{weight, weight_stride, vocab, width}, h{hidden, hidden_stride, n_rows, width};
   const bool fast = direct<int8_t, Load::Rows>(w, width) && direct<int8_t, Load::Rows>(h, width);
-  const Shape s = fast ? shape_of(vocab, n_rows) : Shape::Simple;
+  const Shape s = fast ? cut_of(vocab, n_rows, width, 1, 1).shape : Shape::Simple;
   if (!product_fits(s, vocab, n_rows, 1)) return CMSD_ERR_ARG;
   if (dtype == CMSD_F32)
     launch_product<int8_t, Load::Rows, Load::Rows>(
