@@ -123,7 +123,9 @@ try:
     _native.bind(*(C.cast(getattr(_lib, f), C.c_void_p).value for f in (
         "cmsd_confidence", "cmsd_confidence_var", "cmsd_draft_len", "cmsd_draft_sample", "cmsd_verify",
         "cmsd_logit_pass", "cmsd_logit_pass_fused")))
-except ImportError as e:
+    _native.bind_head(*(C.cast(getattr(_lib, f), C.c_void_p).value for f in (
+        "cmsd_quantize_rows", "cmsd_head_logits", "cmsd_head_loss", "cmsd_head_loss_grad")))
+except (ImportError, AttributeError) as e:
     _native = None
     warnings.warn(f"no native argument marshalling ({e}): small calls take 6 to 20 us more of host time; "
                   "`python -m paper_2508_15371_amd.build` builds it", RuntimeWarning, stacklevel=2)
@@ -567,6 +569,12 @@ def _launch_on(fn: str, device: torch.device, stream, *args) -> None:
         _check(fn, getattr(_lib, fn)(*args, _stream(stream)))
 
 
+def _native_here(t: torch.Tensor) -> bool:
+    """Whether the native marshalling takes a call on ``t``'s device: it launches on the
+    current one."""
+    return _native is not None and t.is_cuda and t.get_device() == torch._C._cuda_getDevice()
+
+
 def _matrix(t: torch.Tensor, name: str, shape: tuple[int, int], dtype: torch.dtype, device: torch.device) -> int:
     """Row stride of a caller's [rows, columns] buffer with unit inner stride whose rows do
     not overlap."""
@@ -594,6 +602,11 @@ def cmsd_quantize_rows(rows: torch.Tensor, codes: torch.Tensor | None = None, sc
     """Rows [n, width] (float32 or bfloat16) to int8 codes [n, width] and float32 scales
     [n]: the largest magnitude of a row stands at 127.  For a head's weight (once) and for
     hidden rows (per call of cmsd_head_logits)."""
+    if codes is not None and scales is not None and _native_here(rows):
+        status = _native.quantize_rows(rows, codes, scales, _raw_stream(stream))
+        if status is not None:
+            _check("cmsd_quantize_rows", status)
+            return codes, scales
     n, W = _width(rows, "rows")
     dev = rows.device
     code = _dtype_code(rows)
@@ -615,6 +628,11 @@ def cmsd_head_logits(hidden: torch.Tensor, hidden_scales: torch.Tensor, weight: 
     """Logit rows [n, vocab] of quantised hidden rows [n, width] and a quantised weight
     [vocab, width] (cmsd_quantize_rows), times ``scale``.  ``dtype`` (float32 or bfloat16)
     is that of the rows made here where ``logits`` is not given."""
+    if logits is not None and _native_here(hidden):
+        status = _native.head_logits(scale, hidden, weight, logits, hidden_scales, weight_scales, _raw_stream(stream))
+        if status is not None:
+            _check("cmsd_head_logits", status)
+            return logits
     n, W = _width(hidden, "hidden")
     V, _ = _width(weight, "weight")
     dev = hidden.device
@@ -676,6 +694,11 @@ def cmsd_head_loss(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Ten
     """Softmax cross entropy of hidden rows [n, width] under a head's weight [vocab, width]
     against labels [n] int32 (negative: no loss) -> (loss float32 [n], lse float32 [n]);
     no logits are kept."""
+    if loss is not None and lse is not None and workspace is not None and _native_here(hidden):
+        status = _native.head_loss(scale, hidden, weight, labels, loss, lse, workspace, _raw_stream(stream))
+        if status is not None:
+            _check("cmsd_head_loss", status)
+            return loss, lse
     n, V, W, dev, code, hst, wst = _head(hidden, weight, labels)
     if loss is None:
         loss = torch.empty(n, dtype=torch.float32, device=dev)
@@ -698,6 +721,12 @@ def cmsd_head_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, labels: torc
     """Gradients of sum_n grad_loss[n] * loss[n] by the hidden rows and the weight, into the
     buffers given (of their shapes and type; None: not computed, at least one is given).
     ``lse`` is cmsd_head_loss's."""
+    if workspace is not None and _native_here(hidden):
+        status = _native.head_loss_grad(scale, hidden, weight, labels, lse, grad_loss, grad_hidden, grad_weight,
+                                        workspace, _raw_stream(stream))
+        if status is not None:
+            _check("cmsd_head_loss_grad", status)
+            return grad_hidden, grad_weight
     n, V, W, dev, code, hst, wst = _head(hidden, weight, labels)
     _buf(lse, "lse", torch.float32, n, dev)
     _buf(grad_loss, "grad_loss", torch.float32, n, dev)

@@ -26,6 +26,10 @@ decltype(&cmsd_draft_sample) f_draft_sample;
 decltype(&cmsd_verify) f_verify;
 decltype(&cmsd_logit_pass) f_logit_pass;
 decltype(&cmsd_logit_pass_fused) f_logit_pass_fused;
+decltype(&cmsd_quantize_rows) f_quantize_rows;
+decltype(&cmsd_head_logits) f_head_logits;
+decltype(&cmsd_head_loss) f_head_loss;
+decltype(&cmsd_head_loss_grad) f_head_loss_grad;
 
 // Arguments in order; ok turns false at the first that does not fit.
 struct Args {
@@ -294,6 +298,136 @@ PyObject* pass(decltype(f_logit_pass) f, PyObject* const* args, Py_ssize_t n) {
 PyObject* logit_pass(PyObject*, PyObject* const* args, Py_ssize_t n) { return pass(f_logit_pass, args, n); }
 PyObject* logit_pass_fused(PyObject*, PyObject* const* args, Py_ssize_t n) { return pass(f_logit_pass_fused, args, n); }
 
+// A [rows, width] matrix on the GPU with unit inner stride whose rows do not overlap.
+struct Matrix {
+  void* p = nullptr;
+  at::ScalarType type = at::kFloat;
+  int64_t n = 0, width = 0, stride = 0;
+  c10::Device dev = c10::Device(c10::kCPU);
+
+  explicit Matrix(Args& a) {
+    const at::Tensor* t = a.tensor();
+    if (!a.ok) return;
+    if (!t->is_cuda() || t->dim() != 2 || t->size(1) < 1 || (t->size(1) > 1 && t->stride(1) != 1) ||
+        (t->size(0) > 1 && t->stride(0) < t->size(1))) {
+      a.ok = false;
+      return;
+    }
+    type = t->scalar_type();
+    n = t->size(0);
+    width = t->size(1);
+    stride = t->stride(0) > width ? t->stride(0) : width;
+    dev = t->device();
+    p = t->data_ptr();
+  }
+  bool logits() const { return type == at::kFloat || type == at::kBFloat16; }
+  int32_t dtype() const { return type == at::kFloat ? CMSD_F32 : CMSD_BF16; }
+  bool is(at::ScalarType want, int64_t rows, int64_t columns, const c10::Device& on) const {
+    return type == want && n == rows && width == columns && dev == on;
+  }
+};
+
+PyObject* quantize_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&] {
+    Args a{args, n};
+    const Matrix x(a), c(a);
+    a.ok = a.ok && x.logits() && c.is(at::kChar, x.n, x.width, x.dev);
+    float* scales = buffer_of<float>(a, x.n, x.dev);
+    void* st = a.stream();
+    return answer(a, [&] {
+      return f_quantize_rows(x.p, x.dtype(), x.n, x.width, x.stride, static_cast<int8_t*>(c.p), c.stride, scales, st);
+    });
+  });
+}
+
+PyObject* head_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&] {
+    Args a{args, n};
+    const float scale = a.number();
+    const Matrix h(a), w(a), z(a);
+    a.ok = a.ok && h.type == at::kChar && w.is(at::kChar, w.n, h.width, h.dev) && z.logits() &&
+           z.is(z.type, h.n, w.n, h.dev);
+    float* hs = buffer_of<float>(a, h.n, h.dev);
+    float* ws = buffer_of<float>(a, w.n, h.dev);
+    void* st = a.stream();
+    return answer(a, [&] {
+      return f_head_logits(static_cast<const int8_t*>(h.p), h.stride, hs, static_cast<const int8_t*>(w.p), w.stride, ws,
+                           scale, h.n, w.n, h.width, z.p, z.dtype(), z.stride, st);
+    });
+  });
+}
+
+PyObject* head_loss(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&] {
+    Args a{args, n};
+    const float scale = a.number();
+    const Matrix h(a), w(a);
+    a.ok = a.ok && h.logits() && w.is(h.type, w.n, h.width, h.dev);
+    int32_t* y = buffer_of<int32_t>(a, h.n, h.dev);
+    float* loss = buffer_of<float>(a, h.n, h.dev);
+    float* lse = buffer_of<float>(a, h.n, h.dev);
+    size_t bytes = 0;
+    void* ws = workspace(a, bytes, h.dev);
+    void* st = a.stream();
+    return answer(a, [&] {
+      return f_head_loss(h.p, h.stride, w.p, w.stride, h.dtype(), y, scale, h.n, w.n, h.width, loss, lse, ws, bytes, st);
+    });
+  });
+}
+
+PyObject* head_loss_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&] {
+    Args a{args, n};
+    const float scale = a.number();
+    const Matrix h(a), w(a);
+    a.ok = a.ok && h.logits() && w.is(h.type, w.n, h.width, h.dev);
+    int32_t* y = buffer_of<int32_t>(a, h.n, h.dev);
+    float* lse = buffer_of<float>(a, h.n, h.dev);
+    float* g = buffer_of<float>(a, h.n, h.dev);
+    void* out[2] = {nullptr, nullptr};
+    int64_t stride[2] = {h.width, h.width};
+    for (int i = 0; i < 2 && a.ok; ++i) {  // by the hidden rows, by the weight; None: not computed
+      if (a.i < a.n && a.a[a.i] == Py_None) {
+        ++a.i;
+        continue;
+      }
+      const Matrix m(a);
+      a.ok = a.ok && m.is(h.type, i == 0 ? h.n : w.n, h.width, h.dev);
+      out[i] = m.p;
+      stride[i] = m.stride;
+    }
+    a.ok = a.ok && (out[0] || out[1]);
+    size_t bytes = 0;
+    void* ws = workspace(a, bytes, h.dev);
+    void* st = a.stream();
+    return answer(a, [&] {
+      return f_head_loss_grad(h.p, h.stride, w.p, w.stride, h.dtype(), y, lse, g, scale, h.n, w.n, h.width, out[0],
+                              stride[0], out[1], stride[1], ws, bytes, st);
+    });
+  });
+}
+
+// The four calls of the vocabulary projection, as bind().
+PyObject* bind_head(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "bind_head takes 4 addresses");
+    return nullptr;
+  }
+  void* p[4];
+  for (int i = 0; i < 4; ++i) {
+    p[i] = PyLong_AsVoidPtr(args[i]);
+    if (!p[i]) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
+      return nullptr;
+    }
+  }
+  f_quantize_rows = reinterpret_cast<decltype(f_quantize_rows)>(p[0]);
+  f_head_logits = reinterpret_cast<decltype(f_head_logits)>(p[1]);
+  f_head_loss = reinterpret_cast<decltype(f_head_loss)>(p[2]);
+  f_head_loss_grad = reinterpret_cast<decltype(f_head_loss_grad)>(p[3]);
+  Py_RETURN_NONE;
+}
+
 // bind(addresses): the entry points' addresses in the library that cmsd.py loaded, in the
 // order below.
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -322,7 +456,9 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define CMSD_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CMSD_METHOD(bind),         CMSD_METHOD(confidence), CMSD_METHOD(confidence_var),
                          CMSD_METHOD(draft_len),    CMSD_METHOD(draft_sample), CMSD_METHOD(verify),
-                         CMSD_METHOD(logit_pass),   CMSD_METHOD(logit_pass_fused), {nullptr, nullptr, 0, nullptr}};
+                         CMSD_METHOD(logit_pass),   CMSD_METHOD(logit_pass_fused), CMSD_METHOD(bind_head),
+                         CMSD_METHOD(quantize_rows), CMSD_METHOD(head_logits), CMSD_METHOD(head_loss),
+                         CMSD_METHOD(head_loss_grad), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

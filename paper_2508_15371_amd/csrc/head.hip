@@ -766,21 +766,58 @@ __global__ __launch_bounds__(256) void k_zero_rows(T* out, int64_t rows, int64_t
     out[at / width * stride + at % width] = from_float<T>(0.f);
 }
 
-// One workgroup per row: its largest magnitude, then its codes.  A code is the whole number
-// next to x / scale (ties to even), with both quotients in double precision: in single a
-// quotient next to a border falls on either side of it.
+// The whole number next to x / s, ties to even, for |x| <= 127.5 s: an estimate that is off by
+// one at most and next to a border only, and its remainder, which fmaf forms exactly (a
+// multiple of a last place of x or s, and under s in magnitude).  s and x are normal numbers
+// or zero.
+__device__ __forceinline__ int whole_quotient(float x, float s, float inverse) {
+  const float q = rintf(x * inverse);
+  const float twice = 2.f * fmaf(-q, s, x);
+  const int n = (int)q, odd = n & 1;
+  return n + (twice > s || (twice == s && odd)) - (twice < -s || (twice == -s && odd));
+}
+
+// One workgroup per row: its largest magnitude, then its codes.  A thread keeps its values
+// of the row's first KEEP passes in registers and reads what is beyond them again.
+// Bound by the row's way to memory and back, twice over a reduction (bf16, width 4096, us:
+// 8 rows 4.9, 4352 rows 17.2 for 53 MB).
 template <typename T>
 __global__ __launch_bounds__(256) void k_quantize(const T* x, int64_t stride, int64_t width, int8_t* codes,
                                                   int64_t code_stride, float* scales) {
+  constexpr int E = 16 / (int)sizeof(T), KEEP = 4, PASS = 256 * E;
   __shared__ float tops[4];
   const int t = threadIdx.x;
   const T* const row = x + blockIdx.x * stride;
+  const auto chunk = [&](int64_t at, T (&v)[E]) {
+    if (at + E <= width) {
+      __builtin_memcpy(v, row + at, 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        v[e] = T{};
+        if (at + e < width) v[e] = row[at + e];
+      }
+    }
+  };
+  T kept[KEEP][E];
+#pragma unroll
+  for (int k = 0; k < KEEP; ++k) chunk(k * PASS + t * E, kept[k]);
   float top = 0.f;
   bool bad = false;
-  for (int64_t i = t; i < width; i += 256) {
-    const float v = fabsf(to_float(row[i]));
-    top = fmaxf(top, v);
-    bad |= !(v < INFINITY);
+  const auto look = [&](const T (&v)[E]) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float a = fabsf(to_float(v[e]));
+      top = fmaxf(top, a);
+      bad |= !(a < INFINITY);
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < KEEP; ++k) look(kept[k]);
+  for (int64_t at = KEEP * PASS + t * E; at < width; at += PASS) {
+    T v[E];
+    chunk(at, v);
+    look(v);
   }
   if (bad) top = INFINITY;
 #pragma unroll
@@ -788,14 +825,36 @@ __global__ __launch_bounds__(256) void k_quantize(const T* x, int64_t stride, in
   if ((t & 63) == 0) tops[t >> 6] = top;
   __syncthreads();
   top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  const bool finite = top < INFINITY;
-  const float scale = finite ? (float)((double)top / 127.0) : NAN;
+  const float scale = top < INFINITY ? top / 127.f : NAN;
   if (t == 0) scales[blockIdx.x] = scale;
+  // rows of small values are raised out of the subnormal numbers, which changes no quotient
+  const float raise = top < 0x1p-60f ? 0x1p80f : 1.f;
+  const float s = top < 0x1p-60f ? (float)((double)scale * 0x1p80) : scale;
+  const float inverse = scale > 0.f ? 1.f / s : 0.f;
+  const bool none = !(scale > 0.f);
   int8_t* const out = codes + blockIdx.x * code_stride;
-  for (int64_t i = t; i < width; i += 256) {
-    double q = 0.0;
-    if (finite && scale > 0.f) q = fmin(fmax(rint((double)to_float(row[i]) / (double)scale), -127.0), 127.0);
-    out[i] = (int8_t)(int)q;
+  const auto put = [&](int64_t at, const T (&v)[E]) {
+    int8_t c[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int q = whole_quotient(none ? 0.f : to_float(v[e]) * raise, s, inverse);
+      c[e] = none ? (int8_t)0 : (int8_t)(q < -127 ? -127 : (q > 127 ? 127 : q));
+    }
+    if (at + E <= width) {
+      __builtin_memcpy(out + at, c, E);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (at + e < width) out[at + e] = c[e];
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < KEEP; ++k)
+    if (k * PASS + t * E < width) put(k * PASS + t * E, kept[k]);
+  for (int64_t at = KEEP * PASS + t * E; at < width; at += PASS) {
+    T v[E];
+    chunk(at, v);
+    put(at, v);
   }
 }
 

@@ -399,6 +399,56 @@ def test_captured_replayed_and_repeated(cm, dtype, n, v, w):
             assert torch.equal(out[f], want[f]), (k, f)
 
 
+def test_native_marshalling_same_calls(cm):
+    # the same calls through the native and the Python marshalling: equal outputs, every
+    # well-formed call is the native one's case, and the same refusals
+    from tests.test_binding import _Recorder
+    h, wt, y, _, _, _, gl = problem(23, 40, 500, 64, F32)
+    gl = torch.from_numpy(gl).to(DEV)
+    ws = cm.head_workspace(40, 500, 64, F32, DEV)
+    keep = cm._native
+    assert keep is not None
+
+    def calls():
+        out = _outs(40, 500, 64, F32)
+        _all(cm, h, wt, y, gl, out, ws)
+        for which in ("grad_hidden", "grad_weight"):
+            one = torch.zeros_like(h if which == "grad_hidden" else wt)
+            cm.cmsd_head_loss_grad(h, wt, y, out["lse"], gl, workspace=ws, **{which: one})
+            out[which] = one
+        torch.cuda.synchronize()
+        errs = []
+        for call in (lambda: cm.cmsd_quantize_rows(h.t(), out["c"], out["s"]),
+                     lambda: cm.cmsd_quantize_rows(h, out["c"][:39], out["s"]),
+                     lambda: cm.cmsd_head_logits(out["c"], out["s"], out["wc"], out["ws"], out["z"], scale=float("nan")),
+                     lambda: cm.cmsd_head_logits(out["c"], out["s"], out["wc"], out["ws"], out["z"].half()),
+                     lambda: cm.cmsd_head_loss(h, wt, y.long(), out["loss"], out["lse"], workspace=ws),
+                     lambda: cm.cmsd_head_loss(h, wt, y, out["loss"], out["lse"], workspace=ws[:1]),
+                     lambda: cm.cmsd_head_loss_grad(h, wt, y, out["lse"], gl, workspace=ws),
+                     lambda: cm.cmsd_head_loss_grad(h, wt, y, out["lse"], gl, out["gw"], workspace=ws)):
+            with pytest.raises(Exception) as e:
+                call()
+            errs.append((type(e.value), str(e.value)))
+        return out, errs
+
+    try:
+        cm._native = _Recorder(keep)
+        native, native_errs = calls()
+        answers = cm._native.answers
+        cm._native = None
+        plain, plain_errs = calls()
+    finally:
+        cm._native = keep
+    assert {f: [s for s in answers[f] if s is not None][0] for f in answers} == dict.fromkeys(
+        ("quantize_rows", "head_logits", "head_loss", "head_loss_grad"), cm.CMSD_OK)
+    assert [s for s in answers["head_loss_grad"]][:3] == [cm.CMSD_OK] * 3
+    for f in native:
+        assert torch.equal(native[f], plain[f]), f
+    # (a workspace that is too small is the library's own refusal in one, the binding's in the other)
+    assert [e[0] for e in native_errs[:5]] == [e[0] for e in plain_errs[:5]]
+    assert native_errs[:5] == plain_errs[:5] and native_errs[6:] == plain_errs[6:]
+
+
 def test_on_another_stream(cm):
     h, wt, y, _, _, _, gl = problem(22, 64, 3000, 256, BF16)
     gl = torch.from_numpy(gl).to(DEV)
