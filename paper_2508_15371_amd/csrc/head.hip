@@ -16,6 +16,7 @@
 namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_anywhere __attribute__((aligned(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -51,7 +52,8 @@ struct Mma;
 template <>
 struct Mma<Bf16> {
   typedef f32x4 Acc;
-  static __device__ __forceinline__ Acc mma(u32x4 a, u32x4 b, Acc c) {
+  static constexpr int PARTS = 1;  // instructions of a step
+  static __device__ __forceinline__ Acc mma(u32x4 a, u32x4 b, Acc c, int) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
                                                    0);
   }
@@ -59,18 +61,17 @@ struct Mma<Bf16> {
 template <>
 struct Mma<float> {
   typedef f32x4 Acc;
-  // a lane's four values stand at k = 4g..4g+3 on both sides; instruction j takes the j-th
-  static __device__ __forceinline__ Acc mma(u32x4 a, u32x4 b, Acc c) {
-    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
-    return c;
+  static constexpr int PARTS = 4;  // a lane's four values stand at k = 4g..4g+3 on both sides; part p takes the p-th
+  static __device__ __forceinline__ Acc mma(u32x4 a, u32x4 b, Acc c, int p) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, a)[p], __builtin_bit_cast(f32x4, b)[p], c, 0, 0,
+                                                0);
   }
 };
 template <>
 struct Mma<int8_t> {
   typedef i32x4 Acc;
-  static __device__ __forceinline__ Acc mma(u32x4 a, u32x4 b, Acc c) {
+  static constexpr int PARTS = 1;
+  static __device__ __forceinline__ Acc mma(u32x4 a, u32x4 b, Acc c, int) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
   }
 };
@@ -258,9 +259,11 @@ __global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g,
       for (int j = 0; j < TL::NI; ++j)
         fb[j] = *reinterpret_cast<const u32x4*>(lb + (wn * TL::NI * 16 + j * 16 + (lane & 15)) * kRowBytes + pos);
 #pragma unroll
-      for (int i = 0; i < TL::MI; ++i)
+      for (int p = 0; p < Mma<T>::PARTS; ++p)
 #pragma unroll
-        for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[i], fb[j], acc[i][j]);
+        for (int i = 0; i < TL::MI; ++i)
+#pragma unroll
+          for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[i], fb[j], acc[i][j], p);
     }
   }
   __syncthreads();  // the epilogue may take the LDS
@@ -285,12 +288,13 @@ __global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g,
 // four k one by one, sixteen rows (four chunks) to a line: quad q at q ^ (k >> 2 & 3).  Lines
 // too short for either take as much of it as they have chunks.
 constexpr int kBufferFlags = 0x00020000;  // a raw buffer of 32-bit words
+constexpr int kBufferNt = 2;
 constexpr uint32_t kNowhere = 0x80000000u;  // past every descriptor
 constexpr int64_t kMostRecords = 0x7fffffff;
 
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
-template <typename T, int ROWS, int WAVES, Load LOAD, int RB>
+template <typename T, int ROWS, int WAVES, Load LOAD, int RB, bool ONCE>
 struct Stream {
   static constexpr int E = 16 / sizeof(T);
   static constexpr int BK = RB / sizeof(T);
@@ -349,7 +353,8 @@ struct Stream {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const uint32_t off = past ? kNowhere : at[i];
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + (wave * N + i) * 1024), 16, off, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + (wave * N + i) * 1024), 16, off, 0, 0,
+                                               ONCE ? kBufferNt : 0);
     }
     base += step;
     records -= step;
@@ -403,7 +408,7 @@ __device__ __forceinline__ void interleave() {
   constexpr int PER_A = LA == Load::Rows ? 1 : (sizeof(T) == 2 ? 2 : 4);
   constexpr int PER_B = LB == Load::Rows ? 1 : (sizeof(T) == 2 ? 2 : 4);
   constexpr int READS = TL::MI * PER_A + TL::NI * PER_B;
-  constexpr int MMAS = TL::MI * TL::NI * (sizeof(T) == 4 ? 4 : 1);
+  constexpr int MMAS = TL::MI * TL::NI * Mma<T>::PARTS;
   constexpr int EACH = MMAS / (READS + 2 * LOADS) > 0 ? MMAS / (READS + 2 * LOADS) : 1;
 #pragma unroll
   for (int i = 0; i < READS; ++i) {
@@ -417,10 +422,12 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-template <typename T, class TL, int RB, int STAGES, Load LA, Load LB, class Epilogue>
+// ONCE: a is read once and does not stay in the last-level cache; its loads are marked so.
+template <typename T, class TL, bool ONCE, Load LA, Load LB, class Epilogue>
 __global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, Grid g, Epilogue e) {
-  typedef Stream<T, TL::BM, TL::WM * TL::WN, LA, RB> SA;
-  typedef Stream<T, TL::BN, TL::WM * TL::WN, LB, RB> SB;
+  constexpr int RB = TL::RB, STAGES = TL::STAGES;
+  typedef Stream<T, TL::BM, TL::WM * TL::WN, LA, RB, ONCE> SA;
+  typedef Stream<T, TL::BN, TL::WM * TL::WN, LB, RB, false> SB;
   constexpr int BK = SA::BK;
   constexpr int STAGE = SA::BYTES + SB::BYTES;
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
@@ -460,9 +467,11 @@ __global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, 
   };
   const auto multiply = [&](int from) {
 #pragma unroll
-    for (int i = 0; i < TL::MI; ++i)
+    for (int p = 0; p < Mma<T>::PARTS; ++p)  // (an accumulator's own next instruction waits for it)
 #pragma unroll
-      for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[from][i], fb[from][j], acc[i][j]);
+      for (int i = 0; i < TL::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[from][i], fb[from][j], acc[i][j], p);
   };
   // A step of 64 bytes of k is multiplied while the next is read.  Where the next lies in
   // the next tile, the workgroup meets before it: that tile has arrived (the STAGES - 2
@@ -501,12 +510,14 @@ __global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, 
 
 // Stores a wave's tile: value(i, j, r) of its lanes to row n0 + n(j), column m0 + m(i) + r of
 // `out`, as far as `left_m` columns and the tile's rows go.  Sixteen rows at a time pass
-// through the wave's own part of the LDS, so that a lane stores 16 bytes and a row's
-// lanes a contiguous run: stored from the accumulators, eight bytes of sixteen rows at a
-// time, a tile of 256 x 256 took a tenth of the time of its products over k = 4096.  (The
-// vectors may start at any element: the memory pipeline takes that.)  A wave's LDS
-// operations are done in their order.  add: to what is there.
-template <typename T, class TL, class F>
+// through the wave's own part of the LDS, so that a lane stores 16 bytes and a row's lanes a
+// contiguous run: stored from the accumulators, eight bytes of sixteen rows at a time, a
+// tile of 256 x 256 took a tenth of the time of its products over k = 4096.  LAST: nothing
+// of the call reads them again, and the stores are marked so, which leaves the operands in
+// the caches (256 x 128256 x 2048 in 8 bits 82 -> 73 us, 576 x 50257 x 768 47 -> 40).  (The vectors may
+// start at any element: the memory pipeline takes that.)  A wave's LDS operations are done
+// in their order.  add: to what is there.
+template <bool LAST, typename T, class TL, class F>
 __device__ __forceinline__ void store_rows(const Place<TL>& w, char* lds, T* out, int64_t stride, int left_m, bool add,
                                            const F& value) {
   constexpr int WIDTH = TL::MI * 16;                        // columns of the wave
@@ -514,7 +525,7 @@ __device__ __forceinline__ void store_rows(const Place<TL>& w, char* lds, T* out
   constexpr int E = 16 / (int)sizeof(T);
   constexpr int BYTES = 16 * WIDTH * (int)sizeof(T);        // of sixteen rows
   static_assert(BYTES * TL::WM * TL::WN <= TL::LDS, "fits the tiles' space");
-  static_assert(BYTES % 1024 == 0 && (CHUNKS & (CHUNKS - 1)) == 0, "whole loads, a power of two of chunks");
+  static_assert((BYTES % 1024 == 0 || BYTES == 512) && (CHUNKS & (CHUNKS - 1)) == 0, "a power of two of chunks");
   char* const mine = lds + (w.wn * TL::WM + w.wm) * BYTES;
   T* const o = out + w.n0 * stride + w.m0;
   const int row = w.lane & 15, g = w.lane >> 4;
@@ -533,7 +544,8 @@ __device__ __forceinline__ void store_rows(const Place<TL>& w, char* lds, T* out
     }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int k = 0; k < BYTES / 1024; ++k) {
+    for (int k = 0; k < (BYTES + 1023) / 1024; ++k) {
+      if (BYTES < 1024 && w.lane >= BYTES / 16) continue;
       const int at = k * 64 + w.lane, r = at / CHUNKS, c = (at % CHUNKS) ^ (r & (CHUNKS - 1));
       T v[E];
       __builtin_memcpy(v, __builtin_assume_aligned(mine + at * 16, 16), 16);
@@ -547,7 +559,12 @@ __device__ __forceinline__ void store_rows(const Place<TL>& w, char* lds, T* out
 #pragma unroll
           for (int e = 0; e < E; ++e) v[e] = from_float<T>(to_float(v[e]) + to_float(u[e]));
         }
-        __builtin_memcpy(p, v, 16);
+        u32x4 x;
+        __builtin_memcpy(&x, v, 16);
+        if constexpr (LAST)
+          __builtin_nontemporal_store(x, reinterpret_cast<u32x4_anywhere*>(p));
+        else
+          *reinterpret_cast<u32x4_anywhere*>(p) = x;
       } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -579,8 +596,8 @@ struct LogitRows {
       }
 #pragma unroll
     for (int j = 0; j < TL::NI; ++j) sh[j] = hidden_scales[w.n0 + (w.n(j) < w.left_n ? w.n(j) : 0)] * scale;
-    store_rows<T>(w, lds, out, stride, w.left_m, false,
-                  [&](int i, int j, int r) { return (float)acc[i][j][r] * sh[j] * sw[i][r]; });
+    store_rows<true>(w, lds, out, stride, w.left_m, false,
+                     [&](int i, int j, int r) { return (float)acc[i][j][r] * sh[j] * sw[i][r]; });
   }
 };
 
@@ -703,24 +720,35 @@ struct LogitGradient {
       return counts[j] ? (at[j] == i * 16 + r ? p - 1.f : p) * g[j] : 0.f;
     };
     if (w.left_m == TL::BM)
-      store_rows<T>(w, lds, out, stride, filled, false, value);
+      store_rows<false>(w, lds, out, stride, filled, false, value);
     else
-      store_rows<T>(w, lds, out, stride, filled, false,
-                    [&](int i, int j, int r) { return w.m(i) + r < w.left_m ? value(i, j, r) : 0.f; });
+      store_rows<false>(w, lds, out, stride, filled, false,
+                        [&](int i, int j, int r) { return w.m(i) + r < w.left_m ? value(i, j, r) : 0.f; });
   }
 };
 
-// A product as it is: rounded to T, or (T = float, slabs) each part of k into a slab of its
-// own, added to what a former piece left there.
+// A product as it is, rounded to T.
 template <typename T>
 struct Plain {
   T* out;
+  int64_t stride;
+
+  template <class TL, class Acc>
+  __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, char* lds) const {
+    store_rows<true>(w, lds, out, stride, w.left_m, false, [&](int i, int j, int r) { return acc[i][j][r]; });
+  }
+};
+
+// Each part of k into a slab of its own, added to what a former piece left there.
+struct Slabs {
+  float* out;
   int64_t stride, slab;
   bool add;
 
   template <class TL, class Acc>
   __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, char* lds) const {
-    store_rows<T>(w, lds, out + w.part * slab, stride, w.left_m, add, [&](int i, int j, int r) { return acc[i][j][r]; });
+    store_rows<false>(w, lds, out + w.part * slab, stride, w.left_m, add,
+                      [&](int i, int j, int r) { return acc[i][j][r]; });
   }
 };
 
@@ -872,24 +900,27 @@ constexpr int64_t kMostWidth = (int64_t)1 << 17;  // an int32 sum of 2^17 - 1 pr
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 
 // The tiles of aligned operands, m (vocabulary or width) by n.
-enum class Shape { Simple, Large, Medium, Low, Few };
+enum class Shape { Simple, Large, Wide, Medium, Low, Few };
 struct LargeTile : Tile<256, 256, 2, 4> {  // one workgroup per compute unit
+  static constexpr int RB = 128, STAGES = 2;
+};
+struct WideTile : Tile<128, 192, 2, 4> {  // two
   static constexpr int RB = 128, STAGES = 2;
 };
 struct MediumTile : Tile<128, 128, 2, 4> {  // two
   static constexpr int RB = 128, STAGES = 2;
 };
-struct LowTile : Tile<128, 64, 2, 2> {
+struct LowTile : Tile<128, 64, 4, 2> {
   static constexpr int RB = 128, STAGES = 3;
 };
-struct FewTile : Tile<128, 32, 4, 1> {
+struct FewTile : Tile<64, 32, 2, 2> {
   static constexpr int RB = 128, STAGES = 4;
 };
-int tile_m(Shape s) { return s == Shape::Large ? 256 : s == Shape::Simple ? 64 : 128; }
+int tile_m(Shape s) { return s == Shape::Large ? 256 : s == Shape::Simple || s == Shape::Few ? 64 : 128; }
 int tile_n(Shape s) {
-  return s == Shape::Large ? 256 : s == Shape::Medium ? 128 : s == Shape::Few ? 32 : 64;
+  return s == Shape::Large ? 256 : s == Shape::Wide ? 192 : s == Shape::Medium ? 128 : s == Shape::Few ? 32 : 64;
 }
-int threads_of(Shape s) { return s == Shape::Large || s == Shape::Medium ? 512 : 256; }
+int threads_of(Shape s) { return s == Shape::Simple || s == Shape::Few ? 256 : 512; }
 
 // Whether a side can be read directly: rows at multiples of 16 bytes, k (of a row-major
 // side; its length, of a transposed one) in whole chunks, a tile's offsets in 31 bits.
@@ -903,8 +934,20 @@ bool direct(const Side& s, int64_t k) {
 
 template <typename T, class TL, Load LA, Load LB, class Epilogue>
 void launch_direct(const Side& a, const Side& b, const Grid& g, unsigned groups, const Epilogue& e, hipStream_t st) {
-  hipLaunchKernelGGL((k_product_direct<T, TL, TL::RB, TL::STAGES, LA, LB, Epilogue>), dim3(groups), dim3(TL::THREADS), 0, st, a,
-                     b, g, e);
+  hipLaunchKernelGGL((k_product_direct<T, TL, false, LA, LB, Epilogue>), dim3(groups), dim3(TL::THREADS), 0, st, a, b, g,
+                     e);
+}
+// Few rows: the weight is read once.  One that the last-level cache (256 MB) holds no large
+// part of is marked so; a smaller one may still lie there from the call before.  8 rows,
+// us without and with the mark: 152064 x 4096 in 8 bits (623 MB) 111 and 102; again and
+// again the same 128256 x 2048 (263 MB) 38 and 42.
+template <typename T, class TL, Load LA, Load LB, class Epilogue>
+void launch_few(const Side& a, const Side& b, const Grid& g, unsigned groups, const Epilogue& e, hipStream_t st) {
+  if (a.rows * g.k * (int64_t)sizeof(T) > (int64_t)384 << 20)
+    hipLaunchKernelGGL((k_product_direct<T, TL, true, LA, LB, Epilogue>), dim3(groups), dim3(TL::THREADS), 0, st, a, b, g,
+                       e);
+  else
+    launch_direct<T, TL, LA, LB>(a, b, g, groups, e, st);
 }
 int64_t product_groups(Shape s, int64_t m, int64_t n, int parts) {
   return ceil_div(m, tile_m(s)) * ceil_div(n, tile_n(s)) * parts;
@@ -915,24 +958,28 @@ struct Cut {
   int parts;
 };
 // Few rows (n) take tiles as low as they are: such a product reads its weight once and is
-// bound by that.  Else large or medium tiles and, where most_parts allows, parts of k, by
-// what they are expected to take: rounds of workgroups over the chip, each round its tiles
-// of 128 bytes of k and a start and an end worth some more, and the slabs of parts written
-// and read.  Measured on 256 compute units, us per tile of k and round: 16-bit and 8-bit
-// types large 1.45, medium 0.92 (two workgroups), 32-bit 7.2 and 3.6 (bound by the matrix
-// cores alike).  16384 x 8192 x 4096, bf16: large 0.77 ms, medium 0.94; 50257 x 1000 x 768
-// 96 and 90 us; 1024 x 4096 over k = 32000 in 1 and 4 parts: large 0.69 and 0.22 ms,
-// medium 0.41 and 0.28.
+// bound by that (4 to 16 waves of a compute unit on it; 16 rows of 32000 x 4096 in bf16,
+// 262 MB, 38 us with tiles of 64 x 32, 40 with 128 x 32, 42 with 256 x 32; 64 rows
+// of 152064 x 4096 in 8 bits 128 us with 128 x 64, 153 with 128 x 128).  Else the tile and, where most_parts allows, the parts of k are those that
+// are expected to take least: rounds of workgroups over the chip, each round its tiles of
+// 128 bytes of k and a start and an end worth some more, and the slabs of parts written and
+// read.  Measured on 256 compute units, us per tile of k and round, and the start and end in
+// tiles of k: large 1.45 and 5, wide 1.21 and 2.5, medium 0.92 and 2 (two workgroups of
+// either on a compute unit); 32 bits, bound by the matrix cores whatever the tile, medium
+// 3.9 and 1 (large spilled registers and was slower, 146 against 143 us for
+// 32000 x 1024 x 256).  bf16, us of large, wide and medium: 16384 x 8192 x 4096 790, 851 and
+// 962; 50257 x 2048 x 768 164, 158 and 173; 50257 x 1000 x 768 92, 94 and 92; 1024 x 4096
+// over k = 32000 684, 464 and 410, in four parts 216, 278 and 280.
 Cut cut_of(int64_t m, int64_t n, int64_t k, int es, int most_parts) {
   const int64_t tiles_k = ceil_div(k * es, kRowBytes);
   if (n <= 64 && most_parts <= 1) return Cut{n <= 32 ? Shape::Few : Shape::Low, 1};
   Cut best{Shape::Medium, 1};
   double least = INFINITY;
-  for (const Shape s : {Shape::Large, Shape::Medium}) {
-    const bool large = s == Shape::Large;
-    const double unit = es == 4 ? (large ? 7.2 : 3.6) : (large ? 1.45 : 0.92);
-    const double more = es == 4 ? 1.0 : (large ? 5.0 : 2.0);
-    const int64_t tiles = product_groups(s, m, n, 1), slots = large ? 256 : 512;
+  for (const Shape s : {Shape::Large, Shape::Wide, Shape::Medium}) {
+    if (es == 4 && s != Shape::Medium) continue;
+    const double unit = es == 4 ? 3.9 : s == Shape::Large ? 1.45 : s == Shape::Wide ? 1.21 : 0.92;
+    const double more = es == 4 ? 1.0 : s == Shape::Large ? 5.0 : s == Shape::Wide ? 2.5 : 2.0;
+    const int64_t tiles = product_groups(s, m, n, 1), slots = s == Shape::Large ? 256 : 512;
     for (int parts = 1; parts <= most_parts && (parts == 1 || tiles_k / parts >= 4); ++parts) {
       const double slabs = parts > 1 ? 2.0 * parts * m * n * 4 / 4e6 : 0.0;
       if (slabs > 250.0) break;
@@ -963,10 +1010,19 @@ void launch_product(Shape s, const Side& a, const Side& b, int64_t k, int parts,
       hipLaunchKernelGGL((k_product<T, SimpleTile, LA, LB, Epilogue>), dim3(groups), dim3(SimpleTile::THREADS), 0, st, a,
                          b, g, e);
       break;
-    case Shape::Large: launch_direct<T, LargeTile, LA, LB>(a, b, g, groups, e, st); break;
+    case Shape::Large:  // 8 and 16 bits (cut_of)
+      if constexpr (sizeof(T) < 4) launch_direct<T, LargeTile, LA, LB>(a, b, g, groups, e, st);
+      break;
+    case Shape::Wide:
+      if constexpr (sizeof(T) < 4) launch_direct<T, WideTile, LA, LB>(a, b, g, groups, e, st);
+      break;
     case Shape::Medium: launch_direct<T, MediumTile, LA, LB>(a, b, g, groups, e, st); break;
-    case Shape::Low: launch_direct<T, LowTile, LA, LB>(a, b, g, groups, e, st); break;
-    case Shape::Few: launch_direct<T, FewTile, LA, LB>(a, b, g, groups, e, st); break;
+    case Shape::Low:  // row-major operands (cut_of)
+      if constexpr (LA == Load::Rows) launch_few<T, LowTile, LA, LB>(a, b, g, groups, e, st);
+      break;
+    case Shape::Few:
+      if constexpr (LA == Load::Rows) launch_few<T, FewTile, LA, LB>(a, b, g, groups, e, st);
+      break;
   }
 }
 
@@ -1081,20 +1137,20 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
       const Side wt{rows, a.weight_stride, a.width, m}, d{dz, p.stride, a.n, k};
       if (slabs)
         launch_product<T, Load::Columns, Load::Rows>(hshape, wt, d, k, p.hidden.parts,
-                                                     Plain<float>{hs, a.width, a.n * a.width, v > 0}, st);
+                                                     Slabs{hs, a.width, a.n * a.width, v > 0}, st);
       else
         launch_product<T, Load::Columns, Load::Rows>(hshape, wt, d, k, 1,
-                                                     Plain<T>{static_cast<T*>(grad_hidden), gh_stride, 0, false}, st);
+                                                     Plain<T>{static_cast<T*>(grad_hidden), gh_stride}, st);
     }
     if (grad_weight) {
       const Side dt{dz, p.stride, m, a.n};
       T* const out = static_cast<T*>(grad_weight) + v * gw_stride;
       if (p.weight.parts > 1) {
         launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, p.weight.parts,
-                                                        Plain<float>{wsl, a.width, m * a.width, false}, st);
+                                                        Slabs{wsl, a.width, m * a.width, false}, st);
         sum_slabs<T>(wsl, p.weight.parts, m * a.width, m, a.width, out, gw_stride, st);
       } else {
-        launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, 1, Plain<T>{out, gw_stride, 0, false}, st);
+        launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, 1, Plain<T>{out, gw_stride}, st);
       }
     }
   }
