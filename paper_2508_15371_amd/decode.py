@@ -13,9 +13,15 @@ trained weights here.  The drafter is the target with seeded weight noise, so th
 two agree often and the drafter's confidence tracks how often (the regime the
 method targets).  ``python -m paper_2508_15371_amd.decode`` prints tokens per
 iteration, draft length and rollback frequency for the Table III settings.
+
+Two options work on the drafter's vocabulary projection: ``--fit STEPS`` fits the
+drafter to the target's tokens first (``cmsd_head_loss`` and its gradients, through the
+head and the trunk), which is what raises the acceptance a drafter gets; ``--head8``
+drafts with the head in 8-bit integers (``cmsd_head_logits``).
 """
 from __future__ import annotations
 
+import argparse
 import copy
 import math
 from dataclasses import dataclass, field
@@ -47,19 +53,37 @@ class TinyLM(torch.nn.Module):
                 "up": w(d, 4 * d, std=d ** -0.5), "down": w(4 * d, d, std=(4 * d) ** -0.5)})
             self.layers.append(blk)
         self.out = w(d, vocab, std=d ** -0.5)
+        self.head8 = None
 
     def perturbed(self, noise: float, seed: int) -> "TinyLM":
         """A copy with N(0, (noise * std(w))^2) added to every weight tensor."""
         m = copy.deepcopy(self)
+        m.head8 = None                               # of the weight before the noise
         g = torch.Generator().manual_seed(seed)
         with torch.no_grad():
             for p in m.parameters():
                 p.add_(torch.randn(p.shape, generator=g).to(p.device) * (noise * float(p.std())))
         return m
 
+    def use_head8(self, rows: int) -> "TinyLM":
+        """Quantise the head; ``head_rows`` takes up to ``rows`` hidden rows from now on."""
+        self.head8 = pipeline.Head8(self.out.detach().t().contiguous(), rows, scale=self.scale, dtype=torch.float32)
+        return self
+
     @torch.no_grad()
     def forward(self, tok: torch.Tensor) -> torch.Tensor:
         """tok [B, T] int64 -> logits [B, T, V] float32 (causal)."""
+        return (self.scale * (self.hidden(tok) @ self.out)).float()
+
+    @torch.no_grad()
+    def head_rows(self, tok: torch.Tensor, pos: torch.Tensor, out: torch.Tensor) -> None:
+        """The logit rows of position pos[b] of every sequence, by the quantised head, into
+        ``out`` [B, V] float32."""
+        rows = self.hidden(tok)[torch.arange(tok.shape[0], device=tok.device), pos]
+        self.head8.logits(rows, out)
+
+    def hidden(self, tok: torch.Tensor) -> torch.Tensor:
+        """tok [B, T] int64 -> what the head takes, [B, T, d]."""
         B, T = tok.shape
         x = self.emb[tok] + self.pos[:T]
         mask = torch.full((T, T), float("-inf"), device=tok.device).triu(1)
@@ -74,8 +98,7 @@ class TinyLM(torch.nn.Module):
             x = x + torch.matmul(a, v).transpose(1, 2).reshape(B, T, self.d) @ blk["o"]
             h = torch.nn.functional.layer_norm(x, (self.d,))
             x = x + torch.nn.functional.gelu(h @ blk["up"]) @ blk["down"]
-        h = torch.nn.functional.layer_norm(x, (self.d,))
-        return (self.scale * (h @ self.out)).float()
+        return torch.nn.functional.layer_norm(x, (self.d,))
 
 
 @dataclass
@@ -132,9 +155,12 @@ class SpeculativeDecoder:
         assert lmax + K + 1 <= tok.shape[1] and lmax + K <= self.max_len
         # drafting: k_max drafter positions per sequence
         for i in range(K):
-            z = self.d(tok[:, :lmax + i])
-            self.dl[:, i] = z[ar, lens + i - 1]
             rows = self.dl[:, i]
+            if self.d.head8 is None:
+                z = self.d(tok[:, :lmax + i])
+                self.dl[:, i] = z[ar, lens + i - 1]
+            else:
+                self.d.head_rows(tok[:, :lmax + i], lens + i - 1, rows)
             cmsd.cmsd_confidence(rows, self.st_step, lambdas=self.p.lambdas, beta_margin=self.p.beta_margin)
             if self.greedy:
                 self.draw.copy_(self.st_step.view(torch.int32)[:, 6])     # the drafter's top token
@@ -197,6 +223,49 @@ class SpeculativeDecoder:
         return [tok[b, L0:L0 + n_new].tolist() for b in range(B)]
 
 
+class DrafterFit:
+    """Fits a drafter to its target's tokens: hidden rows of random token sequences, the
+    target's top token at each position as the label, the head's loss and both its
+    gradients from the library, the trunk's from autograd behind them; AdamW."""
+
+    def __init__(self, drafter: TinyLM, target: TinyLM, B: int = 64, T: int = 64, lr: float = 1e-4, seed: int = 0,
+                 trunk: bool = True):
+        self.d, self.t, self.B, self.T = drafter, target, B, T
+        self.dev = drafter.out.device
+        drafter.head8 = None                         # quantised again after fitting, if at all
+        self.weight = torch.nn.Parameter(drafter.out.detach().t().contiguous())     # a row per vocabulary entry
+        self.trunk = [p for n, p in drafter.named_parameters() if n != "out"] if trunk else []
+        self.opt = torch.optim.AdamW([self.weight, *self.trunk], lr=lr, weight_decay=0.0)
+        self.head = pipeline.HeadLoss(B * T, drafter.vocab, drafter.d, self.dev, scale=drafter.scale, hidden=trunk)
+        self.grad_loss = torch.full((B * T,), 1.0 / (B * T), device=self.dev)       # the mean over the rows
+        self.gen = torch.Generator(device=self.dev).manual_seed(seed)
+
+    def batch(self) -> tuple[torch.Tensor, torch.Tensor]:
+        """Token sequences [B, T] and the target's top token after each position [B*T] int32."""
+        tok = torch.randint(0, self.d.vocab, (self.B, self.T), generator=self.gen, device=self.dev)
+        return tok, self.t(tok).argmax(-1).view(-1).int()
+
+    def gradients(self, tok: torch.Tensor, labels: torch.Tensor) -> torch.Tensor:
+        """Sets every parameter's gradient of the mean loss; returns the rows' losses."""
+        self.opt.zero_grad(set_to_none=True)
+        with torch.set_grad_enabled(bool(self.trunk)):
+            h = self.d.hidden(tok).reshape(-1, self.d.d)
+        rows = h.detach()
+        loss = self.head.forward(rows, self.weight.detach(), labels)
+        self.head.backward(rows, self.weight.detach(), labels, self.grad_loss)
+        self.weight.grad = self.head.grad_weight
+        if self.trunk:
+            h.backward(self.head.grad_hidden)
+        return loss
+
+    def step(self) -> torch.Tensor:
+        loss = self.gradients(*self.batch())
+        self.opt.step()
+        with torch.no_grad():
+            self.d.out.copy_(self.weight.t())
+        return loss
+
+
 def greedy_reference(target: TinyLM, prompt: torch.Tensor, n_new: int) -> tuple[list, list]:
     """The target's own greedy decode (lowest index among equal maxima) and, per
     step, the gap between its two largest logits."""
@@ -210,9 +279,15 @@ def greedy_reference(target: TinyLM, prompt: torch.Tensor, n_new: int) -> tuple[
     return [tok[b, prompt.shape[1]:].tolist() for b in range(prompt.shape[0])], gaps
 
 
-def _report(device="cuda:0", B=16, k_max=8, V=32000, n_new=96, seed=0, noise=0.1) -> list:
+def _report(device="cuda:0", B=16, k_max=8, V=32000, n_new=96, seed=0, noise=0.1, fit=0, head8=False) -> list:
     target = TinyLM(V, seed=seed + 1).to(device)
     drafter = target.perturbed(noise, seed + 2).to(device)
+    if fit:
+        f = DrafterFit(drafter, target, seed=seed + 3)
+        means = [f.step().mean() for _ in range(fit)]
+        print(f"fitted in {fit} steps: mean loss {float(means[0]):.4f} -> {float(means[-1]):.4f}")
+    if head8:
+        drafter.use_head8(B)
     prompt = torch.randint(0, V, (B, 16), generator=torch.Generator().manual_seed(seed)).to(device)
     base = pipeline.Params()
     settings = [
@@ -239,7 +314,11 @@ def _report(device="cuda:0", B=16, k_max=8, V=32000, n_new=96, seed=0, noise=0.1
 
 
 if __name__ == "__main__":
-    rows = _report()
+    ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
+    ap.add_argument("--fit", type=int, default=0, metavar="STEPS", help="fit the drafter to the target's tokens first")
+    ap.add_argument("--head8", action="store_true", help="draft with the head in 8-bit integers")
+    args = ap.parse_args()
+    rows = _report(fit=args.fit, head8=args.head8)
     print(f"{'setting':34s} {'tok/iter':>8s} {'mean k':>7s} {'accept':>7s} {'rollback':>8s}")
     for r in rows:
         print(f"{r['setting']:34s} {r['tokens_per_iteration']:8.3f} {r['mean_draft_len']:7.2f} "

@@ -124,3 +124,54 @@ class LogitPass:
                                    adaptive=adaptive, draft_stats=self.stats, draft_len=self.k,
                                    target_stats=self.tstats, n_accepted=self.n_acc, next_token=self.next_tok,
                                    workspace=self.fws, stream=stream)
+
+
+class Head8:
+    """A head's weight [vocab, width] in 8-bit codes, and the buffers of its calls for up to
+    ``rows`` hidden rows: the logit rows that the other calls read, in ``dtype``, from a
+    weight of a quarter of the bytes of float32."""
+
+    def __init__(self, weight: torch.Tensor, rows: int, scale: float = 1.0, dtype: torch.dtype = torch.bfloat16):
+        self.scale, self.dtype = float(scale), dtype
+        self.codes, self.scales = cmsd.cmsd_quantize_rows(weight)
+        self.vocab, self.width = weight.shape
+        self.hidden_codes = torch.empty((rows, self.width), dtype=torch.int8, device=weight.device)
+        self.hidden_scales = torch.empty(rows, dtype=torch.float32, device=weight.device)
+
+    def logits(self, hidden: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """hidden [n, width] (n <= rows; float32 or bfloat16) -> logit rows [n, vocab], into
+        ``out`` where given (float32 or bfloat16 rows of any stride)."""
+        n = hidden.shape[0]
+        if n > self.hidden_scales.numel():
+            raise ValueError(f"hidden has {n} rows; this head's buffers hold {self.hidden_scales.numel()}")
+        codes, scales = self.hidden_codes[:n], self.hidden_scales[:n]
+        cmsd.cmsd_quantize_rows(hidden, codes, scales, stream=stream)
+        if out is None:
+            out = torch.empty((n, self.vocab), dtype=self.dtype, device=hidden.device)
+        return cmsd.cmsd_head_logits(codes, scales, self.codes, self.scales, out, scale=self.scale, stream=stream)
+
+
+class HeadLoss:
+    """The softmax cross entropy of ``rows`` hidden rows under a head and its gradients, on
+    buffers that are kept (``hidden``, ``weight``: which gradients)."""
+
+    def __init__(self, rows: int, vocab: int, width: int, device, dtype: torch.dtype = torch.float32,
+                 scale: float = 1.0, hidden: bool = True, weight: bool = True):
+        dev = torch.device(device)
+        self.scale = float(scale)
+        self.loss = torch.empty(rows, dtype=torch.float32, device=dev)
+        self.lse = torch.empty(rows, dtype=torch.float32, device=dev)
+        self.grad_hidden = torch.empty((rows, width), dtype=dtype, device=dev) if hidden else None
+        self.grad_weight = torch.empty((vocab, width), dtype=dtype, device=dev) if weight else None
+        self.ws = cmsd.head_workspace(rows, vocab, width, dtype, dev, grad=hidden or weight)
+
+    def forward(self, hidden, weight, labels, stream=None) -> torch.Tensor:
+        """The rows' losses (0 for a negative label)."""
+        cmsd.cmsd_head_loss(hidden, weight, labels, self.loss, self.lse, scale=self.scale, workspace=self.ws,
+                            stream=stream)
+        return self.loss
+
+    def backward(self, hidden, weight, labels, grad_loss, stream=None) -> None:
+        """The gradients of (grad_loss * loss).sum(), after ``forward`` on the same rows."""
+        cmsd.cmsd_head_loss_grad(hidden, weight, labels, self.lse, grad_loss, self.grad_hidden, self.grad_weight,
+                                 scale=self.scale, workspace=self.ws, stream=stream)

@@ -149,3 +149,11 @@ def test_binding_refuses_types():
         cm.cmsd_head_loss(_f(3, 8, dtype=torch.float64), _f(5, 8, dtype=torch.float64), _f(3, dtype=I32))
     with pytest.raises(TypeError):
         cm.cmsd_head_logits(_f(3, 8, dtype=I8), _f(3), _f(5, 8, dtype=I8), _f(5), dtype=torch.float16)
+
+
+def test_head8_refuses_more_rows_than_its_buffers():
+    from paper_2508_15371_amd import pipeline
+    h = object.__new__(pipeline.Head8)
+    h.hidden_scales, h.hidden_codes = _f(4), _f(4, 8, dtype=I8)
+    with pytest.raises(ValueError, match="5 rows"):
+        h.logits(_f(5, 8))
