@@ -714,16 +714,20 @@ struct LogitGradient {
       less[j] = -lse[n] * kLog2e;
       at[j] = near(label - first, w);
     }
+    bool label_here = false;
+#pragma unroll
+    for (int j = 0; j < TL::NI; ++j) label_here |= at[j] >= 0;
     const int filled = (w.left_m + kPad - 1) / kPad * kPad;
-    const auto value = [&](int i, int j, int r) {
-      const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], mul, less[j]));
-      return counts[j] ? (at[j] == i * 16 + r ? p - 1.f : p) * g[j] : 0.f;
+    const auto apart = [&](int i, int j, int r) {  // a tile without its rows' labels: most are
+      return counts[j] ? __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], mul, less[j])) * g[j] : 0.f;
     };
-    if (w.left_m == TL::BM)
-      store_rows<false>(w, lds, out, stride, filled, false, value);
+    if (w.left_m == TL::BM && !__any(label_here))
+      store_rows<false>(w, lds, out, stride, filled, false, apart);
     else
-      store_rows<false>(w, lds, out, stride, filled, false,
-                        [&](int i, int j, int r) { return w.m(i) + r < w.left_m ? value(i, j, r) : 0.f; });
+      store_rows<false>(w, lds, out, stride, filled, false, [&](int i, int j, int r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], mul, less[j]));
+        return counts[j] && w.m(i) + r < w.left_m ? (at[j] == i * 16 + r ? p - 1.f : p) * g[j] : 0.f;
+      });
   }
 };
 
@@ -981,6 +985,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, int es, int most_parts) {
     const double more = es == 4 ? 1.0 : s == Shape::Large ? 5.0 : s == Shape::Wide ? 2.5 : 2.0;
     const int64_t tiles = product_groups(s, m, n, 1), slots = s == Shape::Large ? 256 : 512;
     for (int parts = 1; parts <= most_parts && (parts == 1 || tiles_k / parts >= 4); ++parts) {
+      if (ceil_div(tiles_k, ceil_div(tiles_k, parts)) < parts) continue;  // a part would be empty
       const double slabs = parts > 1 ? 2.0 * parts * m * n * 4 / 4e6 : 0.0;
       if (slabs > 250.0) break;
       const double us = ceil_div(tiles * parts, slots) * (ceil_div(tiles_k, parts) + more) * unit + slabs;
