@@ -679,9 +679,14 @@ def _head(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor) -> t
     return n, V, W, dev, code, hst, wst
 
 
-def _scratch(workspace: torch.Tensor | None, least: int, device: torch.device) -> torch.Tensor:
+def _scratch(workspace: torch.Tensor | None, least: int, device: torch.device, stream) -> torch.Tensor:
+    """The caller's workspace, or one for this call alone: kept from other uses until the
+    call's stream has passed it."""
     if workspace is None:
-        return torch.empty((max(16, least) + 7) // 8, dtype=torch.float64, device=device)
+        ws = torch.empty((max(16, least) + 7) // 8, dtype=torch.float64, device=device)
+        if stream is not None and ws.is_cuda:
+            ws.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device))
+        return ws
     _buf(workspace, "workspace", workspace.dtype, 0, device)
     if workspace.numel() * workspace.element_size() < least:
         raise ValueError(f"workspace has {workspace.numel() * workspace.element_size()} bytes; {least} are needed")
@@ -706,7 +711,7 @@ def cmsd_head_loss(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Ten
         lse = torch.empty(n, dtype=torch.float32, device=dev)
     _buf(loss, "loss", torch.float32, n, dev)
     _buf(lse, "lse", torch.float32, n, dev)
-    ws = _scratch(workspace, cmsd_head_loss_workspace_bytes(n, V), dev)
+    ws = _scratch(workspace, cmsd_head_loss_workspace_bytes(n, V), dev, stream)
     _on_device(hidden, "hidden")
     _launch_on("cmsd_head_loss", dev, stream, _ptr(hidden), hst, _ptr(weight), wst, code, _ptr(labels), float(scale), n,
                V, W, _ptr(loss), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size())
@@ -737,7 +742,7 @@ def cmsd_head_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, labels: torc
         ghst = _matrix(grad_hidden, "grad_hidden", (n, W), hidden.dtype, dev)
     if grad_weight is not None:
         gwst = _matrix(grad_weight, "grad_weight", (V, W), hidden.dtype, dev)
-    ws = _scratch(workspace, cmsd_head_loss_grad_workspace_bytes(n, V, W, hidden.dtype), dev)
+    ws = _scratch(workspace, cmsd_head_loss_grad_workspace_bytes(n, V, W, hidden.dtype), dev, stream)
     _on_device(hidden, "hidden")
     _launch_on("cmsd_head_loss_grad", dev, stream, _ptr(hidden), hst, _ptr(weight), wst, code, _ptr(labels), _ptr(lse),
                _ptr(grad_loss), float(scale), n, V, W, _ptr(grad_hidden), ghst, _ptr(grad_weight), gwst, _ptr(ws),

@@ -196,7 +196,6 @@ struct Place {
   int tile_m, part;
   __device__ __forceinline__ int m(int i) const { return wm * TL::MI * 16 + i * 16 + (lane >> 4) * 4; }
   __device__ __forceinline__ int n(int j) const { return wn * TL::NI * 16 + j * 16 + (lane & 15); }
-  __device__ __forceinline__ bool whole() const { return left_m == TL::BM && left_n == TL::BN; }
 };
 template <class TL>
 __device__ __forceinline__ Place<TL> place_of(const TileAt& q, int64_t M, int64_t N, int wm, int wn, int lane, int t) {
@@ -294,12 +293,11 @@ constexpr int64_t kMostRecords = 0x7fffffff;
 
 typedef __attribute__((address_space(3))) void* LdsPtr;
 
-template <typename T, int ROWS, int WAVES, Load LOAD, int RB, bool ONCE>
+template <typename T, int ROWS, int WAVES, Load LOAD, bool ONCE>
 struct Stream {
   static constexpr int E = 16 / sizeof(T);
-  static constexpr int BK = RB / sizeof(T);
-  static constexpr int CHUNKS = RB / 16;
-  static constexpr int BYTES = ROWS * RB;
+  static constexpr int BK = kRowBytes / sizeof(T);
+  static constexpr int BYTES = ROWS * kRowBytes;
   static constexpr int N = BYTES / 1024 / WAVES;  // loads of a wave per tile
   static_assert(N * WAVES * 1024 == BYTES, "whole loads per wave");
   static constexpr int LINE = ROWS * (int)sizeof(T);  // bytes of one k of a transposed side
@@ -309,7 +307,6 @@ struct Stream {
   int64_t records;  // bytes from base to the side's end
   uint32_t at[N];
 
-  static __device__ __forceinline__ int turn(int row) { return RB == 128 ? row & 7 : (row >> 1) & 3; }
   static __device__ __forceinline__ int swizzle(int k) {
     return (sizeof(T) == 2 ? ((k & 3) | ((k >> 1) & 4)) << 1 : ((k >> 2) & 3) << 2) & (LINE / 16 - 1);
   }
@@ -319,7 +316,7 @@ struct Stream {
     const char* p = static_cast<const char*>(s.p);
     if (LOAD == Load::Rows) {
       base = p + row0 * stride + k0 * (int64_t)sizeof(T);
-      step = RB;
+      step = kRowBytes;
       const int64_t rows = s.rows - row0 < ROWS ? s.rows - row0 : ROWS;
       records = (rows - 1) * stride + (k_end - k0) * (int64_t)sizeof(T);
     } else {
@@ -334,7 +331,7 @@ struct Stream {
     for (int i = 0; i < N; ++i) {
       const int pos = (wave * N + i) * 64 + lane;  // 16-byte position in the tile
       if (LOAD == Load::Rows) {
-        const int row = pos / CHUNKS, c = (pos % CHUNKS) ^ turn(row);
+        const int row = pos / kChunks, c = (pos % kChunks) ^ (row & 7);
         at[i] = (uint32_t)(row * stride + c * 16);
       } else {
         const int k = pos / (LINE / 16), c = (pos % (LINE / 16)) ^ swizzle(k);
@@ -349,7 +346,7 @@ struct Stream {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<char*>(base), 0, __builtin_amdgcn_readfirstlane(left > 0 ? (int)n : 0), kBufferFlags);
     // a lane's chunk of its rows is the same in all its loads: they are 1024 bytes apart
-    const bool past = LOAD == Load::Rows && ((lane % CHUNKS) ^ turn(lane / CHUNKS)) * E >= left;
+    const bool past = LOAD == Load::Rows && ((lane % kChunks) ^ (lane / kChunks)) * E >= left;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const uint32_t off = past ? kNowhere : at[i];
@@ -365,7 +362,7 @@ struct Stream {
   static __device__ __forceinline__ u32x4 fragment(const char* __restrict lds, int row0, int s, int lane) {
     const int g = lane >> 4, r = lane & 15;
     if (LOAD == Load::Rows)
-      return *reinterpret_cast<const u32x4*>(lds + (row0 + r) * RB + (((s * 4 + g) ^ turn(r)) << 4));
+      return *reinterpret_cast<const u32x4*>(lds + (row0 + r) * kRowBytes + (((s * 4 + g) ^ (r & 7)) << 4));
     if constexpr (sizeof(T) == 2) {
       typedef __attribute__((ext_vector_type(4))) short s16x4;
       typedef __attribute__((address_space(3))) s16x4* P;
@@ -425,9 +422,9 @@ __device__ __forceinline__ void interleave() {
 // ONCE: a is read once and does not stay in the last-level cache; its loads are marked so.
 template <typename T, class TL, bool ONCE, Load LA, Load LB, class Epilogue>
 __global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, Grid g, Epilogue e) {
-  constexpr int RB = TL::RB, STAGES = TL::STAGES;
-  typedef Stream<T, TL::BM, TL::WM * TL::WN, LA, RB, ONCE> SA;
-  typedef Stream<T, TL::BN, TL::WM * TL::WN, LB, RB, false> SB;
+  constexpr int STAGES = TL::STAGES;
+  typedef Stream<T, TL::BM, TL::WM * TL::WN, LA, ONCE> SA;
+  typedef Stream<T, TL::BN, TL::WM * TL::WN, LB, false> SB;
   constexpr int BK = SA::BK;
   constexpr int STAGE = SA::BYTES + SB::BYTES;
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
@@ -459,50 +456,39 @@ __global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, 
     left -= BK;
   }
   u32x4 fa[2][TL::MI], fb[2][TL::NI];
-  const auto read = [&](int to, int half, const char* tile) {
+  const auto read = [&](int half, const char* tile) {
 #pragma unroll
-    for (int i = 0; i < TL::MI; ++i) fa[to][i] = SA::fragment(tile, wm * TL::MI * 16 + i * 16, half, lane);
+    for (int i = 0; i < TL::MI; ++i) fa[half][i] = SA::fragment(tile, wm * TL::MI * 16 + i * 16, half, lane);
 #pragma unroll
-    for (int j = 0; j < TL::NI; ++j) fb[to][j] = SB::fragment(tile + SA::BYTES, wn * TL::NI * 16 + j * 16, half, lane);
+    for (int j = 0; j < TL::NI; ++j) fb[half][j] = SB::fragment(tile + SA::BYTES, wn * TL::NI * 16 + j * 16, half, lane);
   };
-  const auto multiply = [&](int from) {
+  const auto multiply = [&](int half) {
 #pragma unroll
     for (int p = 0; p < Mma<T>::PARTS; ++p)  // (an accumulator's own next instruction waits for it)
 #pragma unroll
       for (int i = 0; i < TL::MI; ++i)
 #pragma unroll
-        for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[from][i], fb[from][j], acc[i][j], p);
+        for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[half][i], fb[half][j], acc[i][j], p);
   };
-  // A step of 64 bytes of k is multiplied while the next is read.  Where the next lies in
-  // the next tile, the workgroup meets before it: that tile has arrived (the STAGES - 2
-  // behind it may be under way), and this one has been read by all, so its space takes a
-  // new one.
-  int stage = 0, done = 0;
-  const auto to_next_tile = [&](int from) {
+  // Half a tile (64 bytes of k) is multiplied while the next half is read.  Before the first
+  // half of the next tile the workgroup meets: that tile has arrived (the STAGES - 2 behind
+  // it may be under way), and this one has been read by all, so its space takes a new one.
+  wait_and_meet<(STAGES - 1) * (SA::N + SB::N)>();
+  if (tiles > 0) read(0, lds);
+  int stage = 0;
+  for (int i = 0; i < tiles; ++i) {
     char* const here = lds + stage * STAGE;
+    read(1, here);
+    multiply(0);
+    interleave<TL, T, LA, LB, 0>();
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     wait_and_meet<(STAGES - 2) * (SA::N + SB::N)>();
-    ++done;
     sa.load(here, left, wave, lane);
     sb.load(here + SA::BYTES, left, wave, lane);
     left -= BK;
-    read(1 - from, 0, lds + stage * STAGE);  // of no use after the last tile
-    multiply(from);
+    read(0, lds + stage * STAGE);  // of no use after the last tile
+    multiply(1);
     interleave<TL, T, LA, LB, SA::N + SB::N>();
-  };
-  wait_and_meet<(STAGES - 1) * (SA::N + SB::N)>();
-  if (tiles > 0) read(0, 0, lds);
-  while (done < tiles) {
-    if constexpr (RB == 128) {
-      read(1, 1, lds + stage * STAGE);
-      multiply(0);
-      interleave<TL, T, LA, LB, 0>();
-      to_next_tile(1);
-    } else {
-      to_next_tile(0);
-      if (done == tiles) break;
-      to_next_tile(1);
-    }
   }
   wait_and_meet<0>();  // the epilogue may take the LDS
   e.template run<TL>(acc, place_of<TL>(q, a.rows, b.rows, wm, wn, lane, t), lds);
@@ -906,19 +892,19 @@ constexpr int64_t kMostStride = (int64_t)1 << 40;
 // The tiles of aligned operands, m (vocabulary or width) by n.
 enum class Shape { Simple, Large, Wide, Medium, Low, Few };
 struct LargeTile : Tile<256, 256, 2, 4> {  // one workgroup per compute unit
-  static constexpr int RB = 128, STAGES = 2;
+  static constexpr int STAGES = 2;
 };
 struct WideTile : Tile<128, 192, 2, 4> {  // two
-  static constexpr int RB = 128, STAGES = 2;
+  static constexpr int STAGES = 2;
 };
 struct MediumTile : Tile<128, 128, 2, 4> {  // two
-  static constexpr int RB = 128, STAGES = 2;
+  static constexpr int STAGES = 2;
 };
 struct LowTile : Tile<128, 64, 4, 2> {
-  static constexpr int RB = 128, STAGES = 3;
+  static constexpr int STAGES = 3;
 };
 struct FewTile : Tile<64, 32, 2, 2> {
-  static constexpr int RB = 128, STAGES = 4;
+  static constexpr int STAGES = 4;
 };
 int tile_m(Shape s) { return s == Shape::Large ? 256 : s == Shape::Simple || s == Shape::Few ? 64 : 128; }
 int tile_n(Shape s) {
@@ -926,14 +912,17 @@ int tile_n(Shape s) {
 }
 int threads_of(Shape s) { return s == Shape::Simple || s == Shape::Few ? 256 : 512; }
 
-// Whether a side can be read directly: rows at multiples of 16 bytes, k (of a row-major
-// side; its length, of a transposed one) in whole chunks, a tile's offsets in 31 bits.
+// Whether a side can be read directly: rows at multiples of 16 bytes, k of a row-major side
+// in whole chunks (so a transposed one's lines are too: `along` is the width in either), and
+// a tile's offsets in 31 bits.  Those of rows that the side has not may pass that and wrap:
+// they give rows of the output that are not stored.  Of a transposed side's 64 lines of a
+// tile every one has to be in range or past it.
 template <typename T, Load LOAD>
-bool direct(const Side& s, int64_t k) {
+bool direct(const Side& s, int64_t along) {
   constexpr int E = 16 / sizeof(T);
-  const int64_t along = LOAD == Load::Rows ? k : s.rows;
-  return ((uintptr_t)s.p & 15) == 0 && s.stride % E == 0 && (LOAD == Load::Columns || along % E == 0) &&
-         s.stride * (int64_t)sizeof(T) < (int64_t)1 << 22;
+  const int64_t most = LOAD == Load::Columns ? 64 : s.rows < 256 ? s.rows : 256;
+  return ((uintptr_t)s.p & 15) == 0 && s.stride % E == 0 && along % E == 0 &&
+         s.stride * (int64_t)sizeof(T) < ((int64_t)1 << 31) / most;
 }
 
 template <typename T, class TL, Load LA, Load LB, class Epilogue>
@@ -1048,10 +1037,12 @@ struct GradPlan {
   size_t logits_at, hidden_at, weight_at, bytes;
 };
 constexpr int64_t kPieceBytes = (int64_t)1 << 28;  // of a piece's logit gradients
+constexpr int64_t kMostPiece = (int64_t)1 << 20;   // entries: 64 of its rows keep their offsets in 31 bits
 GradPlan grad_plan(int64_t n, int64_t vocab, int64_t width, int es) {
   GradPlan p;
   p.piece = kPieceBytes / (n * es) / 256 * 256;
   if (p.piece < 256) p.piece = 256;
+  if (p.piece > kMostPiece) p.piece = kMostPiece;
   if (p.piece > vocab) p.piece = vocab;
   p.stride = round_up(p.piece, 128);
   p.hidden = cut_of(width, n, p.piece, es, 64);
@@ -1125,7 +1116,8 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
   const Side h{a.hidden, a.hidden_stride, a.n, a.width}, ht{a.hidden, a.hidden_stride, a.width, a.n};
   const Side w0{a.weight, a.weight_stride, a.vocab, a.width};
   // the workspace's rows are aligned, and so are the operands' pieces where the operands are
-  const bool fast = direct<T, Load::Rows>(w0, a.width) && direct<T, Load::Rows>(h, a.width);
+  const bool fast = direct<T, Load::Rows>(w0, a.width) && direct<T, Load::Rows>(h, a.width) &&
+                    direct<T, Load::Columns>(w0, a.width) && direct<T, Load::Columns>(h, a.width);
   const Shape zs = fast ? cut_of(p.piece, a.n, a.width, sizeof(T), 1).shape : Shape::Simple;
   const Shape hshape = fast ? p.hidden.shape : Shape::Simple, wshape = fast ? p.weight.shape : Shape::Simple;
   if (!product_fits(zs, p.piece, a.n, 1) || (grad_hidden && !product_fits(hshape, a.width, a.n, p.hidden.parts)) ||

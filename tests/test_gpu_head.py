@@ -467,6 +467,68 @@ def test_on_another_stream(cm):
         assert torch.equal(got[f], want[f]), f
 
 
+def test_own_workspace_on_another_stream(cm):
+    # a workspace made for the call is not handed out again before its stream has passed it
+    n, v, w = 512, 20000, 256
+    h, wt, y, _, _, _, gl = problem(24, n, v, w, BF16)
+    gl = torch.from_numpy(gl).to(DEV)
+    want, want_lse = cm.cmsd_head_loss(h, wt, y)
+    gh, gw = torch.empty_like(h), torch.empty_like(wt)
+    cm.cmsd_head_loss_grad(h, wt, y, want_lse, gl, gh, gw)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    loss, lse, gh2, gw2 = torch.empty_like(want), torch.empty_like(want), torch.empty_like(h), torch.empty_like(wt)
+    torch.cuda.synchronize()
+    for stream in (s, s.cuda_stream):
+        cm.cmsd_head_loss(h, wt, y, loss, lse, stream=stream)
+        junk = [torch.full((cm.cmsd_head_loss_workspace_bytes(n, v) // 4,), float("nan"), device=DEV) for _ in range(3)]
+        cm.cmsd_head_loss_grad(h, wt, y, want_lse, gl, gh2, gw2, stream=stream)
+        size = cm.cmsd_head_loss_grad_workspace_bytes(n, v, w, BF16)
+        junk += [torch.full((size // 4,), float("nan"), device=DEV) for _ in range(3)]
+        torch.cuda.synchronize()
+        del junk
+        for a, b in ((loss, want), (lse, want_lse), (gh2, gh), (gw2, gw)):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("far", [9_000_000, 40_000_000])
+def test_rows_far_apart(cm, dtype, far):
+    # the last position of long sequences: rows 18 to 160 MB apart
+    n, v, w = 9, 1200, 64
+    h, wt, y, _, _, _, gl = problem(25, n, v, w, dtype)
+    gl = torch.from_numpy(gl).to(DEV)
+    flat = torch.empty(n * far, dtype=dtype, device=DEV)
+    hs = flat.as_strided((n, w), (far, 1))
+    hs.copy_(h)
+    loss, lse = cm.cmsd_head_loss(hs, wt, y)
+    gh, gw = flat.as_strided((n, w), (far, 1), 128), torch.empty_like(wt)
+    cm.cmsd_head_loss_grad(hs, wt, y, lse, gl, gh, gw)
+    for got, (ref, bound), what in zip((loss, lse, gh, gw), _on_gpu(h, wt, y, gl, 1.0, dtype),
+                                       ("loss", "lse", "grad_hidden", "grad_weight")):
+        assert float(((got.double() - ref).abs() / bound).max()) <= 1, what
+    c, s = cm.cmsd_quantize_rows(hs)
+    wc, ws = cm.cmsd_quantize_rows(wt)
+    cs = torch.empty(n * far, dtype=torch.int8, device=DEV).as_strided((n, w), (far, 1))
+    cs.copy_(c)
+    assert torch.equal(cm.cmsd_head_logits(cs, s, wc, ws), cm.cmsd_head_logits(c, s, wc, ws))
+
+
+def test_more_entries_than_a_piece(cm):
+    # few rows, more entries than a piece takes: the second piece is 300 entries
+    n, v, w = 3, (1 << 20) + 300, 16
+    for dtype in (F32, BF16):
+        h, wt, y, _, _, _, gl = problem(26, n, v, w, dtype)
+        y[1], y[2] = v - 1, (1 << 20) - 1
+        gl = torch.from_numpy(np.abs(gl) + 0.1).to(DEV)
+        loss, lse = cm.cmsd_head_loss(h, wt, y)
+        gh, gw = torch.empty_like(h), torch.empty_like(wt)
+        cm.cmsd_head_loss_grad(h, wt, y, lse, gl, gh, gw)
+        for got, (ref, bound), what in zip((loss, lse, gh, gw), _on_gpu(h, wt, y, gl, 1.0, dtype),
+                                           ("loss", "lse", "grad_hidden", "grad_weight")):
+            assert float(((got.double() - ref).abs() / bound).max()) <= 1, (dtype, what)
+
+
 def test_outputs_past_32_bit_offsets(cm):
     # 5.1 GB of logits and a weight of 2.6e9 elements: the last rows against a small call
     n, v, w = 20000, 128256, 16
