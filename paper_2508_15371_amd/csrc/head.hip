@@ -112,50 +112,6 @@ __device__ __forceinline__ u32x4 row_chunk(const T* p, int64_t left) {
   return v;
 }
 
-// The chunks of one side's tile that a thread brings: into registers, then into LDS.
-// Chunk c of row r lies at position c ^ (r & 7) of the row's eight: the sixteen lanes that
-// read one chunk of sixteen rows then take every bank alike.
-template <typename T, int ROWS, int THREADS, Load LOAD>
-struct Bring {
-  static constexpr int E = 16 / sizeof(T);
-  static constexpr int N = ROWS * kChunks / THREADS;
-  static_assert(N * THREADS == ROWS * kChunks, "whole chunks per thread");
-  u32x4 v[N];
-
-  __device__ __forceinline__ void load(const Side& s, int64_t row0, int64_t k0, int64_t k_end, int t) {
-    const T* p = static_cast<const T*>(s.p);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int at = i * THREADS + t;
-      v[i] = u32x4{0u, 0u, 0u, 0u};
-      if (LOAD == Load::Rows) {
-        const int64_t row = row0 + at / kChunks, k = k0 + (at % kChunks) * E;
-        if (row < s.rows && k < k_end) v[i] = row_chunk<T>(p + row * s.stride + k, k_end - k);
-      } else {
-        const int64_t row = row0 + at % ROWS, k = k0 + (at / ROWS) * E;
-        if (row < s.rows) {
-          T x[E];
-#pragma unroll
-          for (int j = 0; j < E; ++j) {
-            x[j] = T{};
-            if (k + j < k_end && k + j < s.k) x[j] = p[(k + j) * s.stride + row];
-          }
-          __builtin_memcpy(&v[i], x, 16);
-        }
-      }
-    }
-  }
-  __device__ __forceinline__ void store(char* lds, int t) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int at = i * THREADS + t;
-      const int row = LOAD == Load::Rows ? at / kChunks : at % ROWS;
-      const int c = LOAD == Load::Rows ? at % kChunks : at / ROWS;
-      *reinterpret_cast<u32x4*>(lds + row * kRowBytes + ((c ^ (row & 7)) << 4)) = v[i];
-    }
-  }
-};
-
 // The tile of a workgroup.  Workgroups go round the eight dies by their number, and each die
 // has an L2 of its own: a die takes a run of tiles, and the run goes through blocks of
 // kBlockM tiles of m by all of n, m first, so that the 32 workgroups a die holds share
@@ -213,88 +169,21 @@ __device__ __forceinline__ Place<TL> place_of(const TileAt& q, int64_t M, int64_
   return w;
 }
 
-template <typename T, class TL, Load LA, Load LB, class Epilogue>
-__global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g, Epilogue e) {
-  constexpr int BK = kRowBytes / sizeof(T);
-  __shared__ __attribute__((aligned(16))) char lds[TL::LDS];
-  char* const la = lds;
-  char* const lb = lds + TL::BM * kRowBytes;
-  const int t = threadIdx.x, lane = t & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int wm = wave % TL::WM, wn = wave / TL::WM;
-
-  const TileAt q = tile_at(g, blockIdx.x);
-  const int64_t m0 = (int64_t)q.m * TL::BM, n0 = (int64_t)q.n * TL::BN;
-  const int64_t k_begin = q.part * g.k_part;
-  const int64_t k_end = k_begin + g.k_part < g.k ? k_begin + g.k_part : g.k;
-
-  typename Mma<T>::Acc acc[TL::MI][TL::NI];
-#pragma unroll
-  for (int i = 0; i < TL::MI; ++i)
-#pragma unroll
-    for (int j = 0; j < TL::NI; ++j) acc[i][j] = typename Mma<T>::Acc{};
-
-  Bring<T, TL::BM, TL::THREADS, LA> ra;
-  Bring<T, TL::BN, TL::THREADS, LB> rb;
-  ra.load(a, m0, k_begin, k_end, t);
-  rb.load(b, n0, k_begin, k_end, t);
-  for (int64_t k = k_begin; k < k_end; k += BK) {
-    __syncthreads();  // the former tile has been read
-    ra.store(la, t);
-    rb.store(lb, t);
-    __syncthreads();
-    if (k + BK < k_end) {
-      ra.load(a, m0, k + BK, k_end, t);
-      rb.load(b, n0, k + BK, k_end, t);
-    }
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 fa[TL::MI], fb[TL::NI];
-      const int pos = ((s * 4 + (lane >> 4)) ^ (lane & 7)) << 4;
-#pragma unroll
-      for (int i = 0; i < TL::MI; ++i)
-        fa[i] = *reinterpret_cast<const u32x4*>(la + (wm * TL::MI * 16 + i * 16 + (lane & 15)) * kRowBytes + pos);
-#pragma unroll
-      for (int j = 0; j < TL::NI; ++j)
-        fb[j] = *reinterpret_cast<const u32x4*>(lb + (wn * TL::NI * 16 + j * 16 + (lane & 15)) * kRowBytes + pos);
-#pragma unroll
-      for (int p = 0; p < Mma<T>::PARTS; ++p)
-#pragma unroll
-        for (int i = 0; i < TL::MI; ++i)
-#pragma unroll
-          for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[i], fb[j], acc[i][j], p);
-    }
-  }
-  __syncthreads();  // the epilogue may take the LDS
-  e.template run<TL>(acc, place_of<TL>(q, a.rows, b.rows, wm, wn, lane, t), lds);
-}
-
-// ------------------------------------------------------- the product of aligned operands
-// The same product where both operands' rows start at multiples of 16 bytes and hold whole
-// 16-byte chunks: the tiles go from memory to LDS directly, a ring of STAGES of them deep,
-// and the workgroup waits for a tile's loads only when it takes the tile.
+// A side's tile in LDS, 128 bytes of k of ROWS rows, brought in by WAVES waves 64 16-byte
+// chunks at a time (load i of a wave fills the 1024 bytes from (wave*N + i)*1024 on).
 //
-// Out of range: a side is read through a buffer descriptor that ends at its last row, and
-// everything past it comes as zeros.  Rows that the tile has too many give rows of the
-// output that are not stored.  For k past its end, a transposed side's rows end there; a
-// row-major side's chunks past it are asked for at an offset past every descriptor.
+// A row-major side: chunk c of row r lies at position c ^ (r & 7) of the row's eight: the
+// sixteen lanes that read one chunk of sixteen rows then take every bank alike.
 //
-// LDS: a row-major side lies as in Bring.  A transposed side (k by k, ROWS values each) is
-// read through the transposing load (16-bit types): sixteen lanes take four k of sixteen
-// rows, 32 bytes of each of the four, and hold four k of a row each afterwards.  Pair of
-// chunks q of line k lies at position q ^ ((k & 3) | (k >> 1 & 4)): the eight lines that
-// thirty-two lanes take stand in banks of their own.  For 32-bit values a lane reads its
-// four k one by one, sixteen rows (four chunks) to a line: quad q at q ^ (k >> 2 & 3).  Lines
-// too short for either take as much of it as they have chunks.
-constexpr int kBufferFlags = 0x00020000;  // a raw buffer of 32-bit words
-constexpr int kBufferNt = 2;
-constexpr uint32_t kNowhere = 0x80000000u;  // past every descriptor
-constexpr int64_t kMostRecords = 0x7fffffff;
-
-typedef __attribute__((address_space(3))) void* LdsPtr;
-
-template <typename T, int ROWS, int WAVES, Load LOAD, bool ONCE>
-struct Stream {
+// A transposed side (k by k, ROWS values each) is read through the transposing load (16-bit
+// types): sixteen lanes take four k of sixteen rows, 32 bytes of each of the four, and hold
+// four k of a row each afterwards.  Pair of chunks q of line k lies at position
+// q ^ ((k & 3) | (k >> 1 & 4)): the eight lines that thirty-two lanes take stand in banks of
+// their own.  For 32-bit values a lane reads its four k one by one, sixteen rows (four
+// chunks) to a line: quad q at q ^ (k >> 2 & 3).  Lines too short for either take as much of
+// it as they have chunks.
+template <typename T, int ROWS, int WAVES, Load LOAD>
+struct Layout {
   static constexpr int E = 16 / sizeof(T);
   static constexpr int BK = kRowBytes / sizeof(T);
   static constexpr int BYTES = ROWS * kRowBytes;
@@ -302,59 +191,21 @@ struct Stream {
   static_assert(N * WAVES * 1024 == BYTES, "whole loads per wave");
   static constexpr int LINE = ROWS * (int)sizeof(T);  // bytes of one k of a transposed side
 
-  const char* base;
-  int64_t step;     // bytes from tile to tile
-  int64_t records;  // bytes from base to the side's end
-  uint32_t at[N];
-
   static __device__ __forceinline__ int swizzle(int k) {
     return (sizeof(T) == 2 ? ((k & 3) | ((k >> 1) & 4)) << 1 : ((k >> 2) & 3) << 2) & (LINE / 16 - 1);
   }
-
-  __device__ __forceinline__ void init(const Side& s, int64_t row0, int64_t k0, int64_t k_end, int wave, int lane) {
-    const int64_t stride = s.stride * (int64_t)sizeof(T);
-    const char* p = static_cast<const char*>(s.p);
+  // What lies at a 16-byte position of the tile: chunk `c` of row (of line k) `r`.
+  struct Spot {
+    int r, c;
+  };
+  static __device__ __forceinline__ Spot spot(int wave, int i, int lane) {
+    const int pos = (wave * N + i) * 64 + lane;
     if (LOAD == Load::Rows) {
-      base = p + row0 * stride + k0 * (int64_t)sizeof(T);
-      step = kRowBytes;
-      const int64_t rows = s.rows - row0 < ROWS ? s.rows - row0 : ROWS;
-      records = (rows - 1) * stride + (k_end - k0) * (int64_t)sizeof(T);
-    } else {
-      k_end = k_end < s.k ? k_end : s.k;
-      base = p + k0 * stride + row0 * (int64_t)sizeof(T);
-      step = BK * stride;
-      // whole chunks: the caller's lines hold them, the workspace's are padded.  (The range
-      // check goes by 32-bit words, and the last line's last 16-bit value must not miss it.)
-      records = (k_end - k0 - 1) * stride + (s.rows - row0 + E - 1) / E * 16;
+      const int r = pos / kChunks;
+      return Spot{r, (pos % kChunks) ^ (r & 7)};
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int pos = (wave * N + i) * 64 + lane;  // 16-byte position in the tile
-      if (LOAD == Load::Rows) {
-        const int row = pos / kChunks, c = (pos % kChunks) ^ (row & 7);
-        at[i] = (uint32_t)(row * stride + c * 16);
-      } else {
-        const int k = pos / (LINE / 16), c = (pos % (LINE / 16)) ^ swizzle(k);
-        at[i] = (uint32_t)(k * stride + c * 16);
-      }
-    }
-  }
-  // The next tile, `left` elements of k from its start to the end (none: zeros come, and no
-  // memory is read).
-  __device__ __forceinline__ void load(char* lds, int left, int wave, int lane) {
-    const int64_t n = records < kMostRecords ? records : kMostRecords;
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<char*>(base), 0, __builtin_amdgcn_readfirstlane(left > 0 ? (int)n : 0), kBufferFlags);
-    // a lane's chunk of its rows is the same in all its loads: they are 1024 bytes apart
-    const bool past = LOAD == Load::Rows && ((lane % kChunks) ^ (lane / kChunks)) * E >= left;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint32_t off = past ? kNowhere : at[i];
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + (wave * N + i) * 1024), 16, off, 0, 0,
-                                               ONCE ? kBufferNt : 0);
-    }
-    base += step;
-    records -= step;
+    const int k = pos / (LINE / 16);
+    return Spot{k, (pos % (LINE / 16)) ^ swizzle(k)};
   }
   // Step s (64 bytes of k) of sixteen rows from row0 of the tile on.  The pointer is said to
   // be the only way to what it reads: the compiler would have the transposing load wait for
@@ -386,6 +237,73 @@ struct Stream {
   }
 };
 
+// ------------------------------------------------------- the product of aligned operands
+// Where both operands' rows start at multiples of 16 bytes and hold whole 16-byte chunks, the
+// tiles go from memory to LDS directly, a ring of STAGES of them deep, and the workgroup
+// waits for a tile's loads only when it takes the tile.
+//
+// Out of range: a side is read through a buffer descriptor that ends at its last row, and
+// everything past it comes as zeros.  Rows that the tile has too many give rows of the
+// output that are not stored.  For k past its end, a transposed side's rows end there; a
+// row-major side's chunks past it are asked for at an offset past every descriptor.
+constexpr int kBufferFlags = 0x00020000;  // a raw buffer of 32-bit words
+constexpr int kBufferNt = 2;
+constexpr uint32_t kNowhere = 0x80000000u;  // past every descriptor
+constexpr int64_t kMostRecords = 0x7fffffff;
+
+typedef __attribute__((address_space(3))) void* LdsPtr;
+
+template <typename T, int ROWS, int WAVES, Load LOAD, bool ONCE>
+struct Stream : Layout<T, ROWS, WAVES, LOAD> {
+  typedef Layout<T, ROWS, WAVES, LOAD> L;
+  using L::BK, L::E, L::N;
+
+  const char* base;
+  int64_t step;     // bytes from tile to tile
+  int64_t records;  // bytes from base to the side's end
+  uint32_t at[N];
+
+  __device__ __forceinline__ void init(const Side& s, int64_t row0, int64_t k0, int64_t k_end, int wave, int lane) {
+    const int64_t stride = s.stride * (int64_t)sizeof(T);
+    const char* p = static_cast<const char*>(s.p);
+    if (LOAD == Load::Rows) {
+      base = p + row0 * stride + k0 * (int64_t)sizeof(T);
+      step = kRowBytes;
+      const int64_t rows = s.rows - row0 < ROWS ? s.rows - row0 : ROWS;
+      records = (rows - 1) * stride + (k_end - k0) * (int64_t)sizeof(T);
+    } else {
+      k_end = k_end < s.k ? k_end : s.k;
+      base = p + k0 * stride + row0 * (int64_t)sizeof(T);
+      step = BK * stride;
+      // whole chunks: the caller's lines hold them, the workspace's are padded.  (The range
+      // check goes by 32-bit words, and the last line's last 16-bit value must not miss it.)
+      records = (k_end - k0 - 1) * stride + (s.rows - row0 + E - 1) / E * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const typename L::Spot x = L::spot(wave, i, lane);
+      at[i] = (uint32_t)(x.r * stride + x.c * 16);
+    }
+  }
+  // The next tile, `left` elements of k from its start to the end (none: zeros come, and no
+  // memory is read).
+  __device__ __forceinline__ void load(char* lds, int left, int wave, int lane) {
+    const int64_t n = records < kMostRecords ? records : kMostRecords;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(base), 0, __builtin_amdgcn_readfirstlane(left > 0 ? (int)n : 0), kBufferFlags);
+    // a lane's chunk of its rows is the same in all its loads: they are 1024 bytes apart
+    const bool past = LOAD == Load::Rows && ((lane % kChunks) ^ (lane / kChunks)) * E >= left;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t off = past ? kNowhere : at[i];
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + (wave * N + i) * 1024), 16, off, 0, 0,
+                                               ONCE ? kBufferNt : 0);
+    }
+    base += step;
+    records -= step;
+  }
+};
+
 // Waits until at most N of the wave's loads are under way and all its LDS reads are done,
 // then for the other waves.
 template <int N>
@@ -396,6 +314,9 @@ __device__ __forceinline__ void wait_and_meet() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+
+// Waits until the wave's LDS operations are done, then for the other waves.
+__device__ __forceinline__ void meet() { wait_and_meet<63>(); }
 
 // The order of a step's instructions: LDS reads (their values are the next step's), then
 // LOADS loads of a further tile, among the products.  A wave issues in order, and a load
@@ -491,6 +412,123 @@ __global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, 
     interleave<TL, T, LA, LB, SA::N + SB::N>();
   }
   wait_and_meet<0>();  // the epilogue may take the LDS
+  e.template run<TL>(acc, place_of<TL>(q, a.rows, b.rows, wm, wn, lane, t), lds);
+}
+
+// ------------------------------------------------------- the product of any operands
+// Operands of any alignment and length pass through registers on their way to LDS, 16 bytes
+// at a time (the memory pipeline takes a vector at any address), the last of a row by its
+// elements.  Two tiles in LDS: one is multiplied while the next is on its way.
+template <typename T, int ROWS, int WAVES, Load LOAD>
+struct Carry : Layout<T, ROWS, WAVES, LOAD> {
+  typedef Layout<T, ROWS, WAVES, LOAD> L;
+  using L::BK, L::E, L::N;
+
+  const T* at[N];
+  int first[N], here[N];  // a chunk's first k of the tile, and how many of its elements the side has
+  int64_t step;
+  int gone;  // of k that the product has and the side has not
+  u32x4 v[N];
+
+  __device__ __forceinline__ void init(const Side& s, int64_t row0, int64_t k0, int64_t k_end, int wave, int lane) {
+    const T* p = static_cast<const T*>(s.p);
+    step = LOAD == Load::Rows ? BK : BK * s.stride;
+    gone = LOAD == Load::Columns && k_end > s.k ? (int)(k_end - s.k) : 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const typename L::Spot x = L::spot(wave, i, lane);
+      if (LOAD == Load::Rows) {
+        at[i] = p + (row0 + x.r) * s.stride + k0 + x.c * E;
+        first[i] = x.c * E;
+        here[i] = row0 + x.r < s.rows ? E : 0;
+      } else {
+        const int64_t row = row0 + x.c * E;
+        at[i] = p + (k0 + x.r) * s.stride + row;
+        first[i] = x.r;
+        here[i] = s.rows - row >= E ? E : (s.rows > row ? (int)(s.rows - row) : 0);
+      }
+    }
+  }
+  // The next tile, `left` elements of k from its start to the end.
+  __device__ __forceinline__ void load(int left) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int n = here[i];  // elements of the chunk
+      if (LOAD == Load::Rows) {
+        if (left < BK && n > 0) n = left - first[i] < E ? left - first[i] : E;
+      } else if (first[i] >= left - gone) {
+        n = 0;
+      }
+      v[i] = n > 0 ? row_chunk<T>(at[i], n) : u32x4{0u, 0u, 0u, 0u};
+      at[i] += step;
+    }
+  }
+  __device__ __forceinline__ void store(char* lds, int wave, int lane) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + ((wave * N + i) * 64 + lane) * 16) = v[i];
+  }
+};
+
+template <typename T, class TL, Load LA, Load LB, class Epilogue>
+__global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g, Epilogue e) {
+  typedef Carry<T, TL::BM, TL::WM * TL::WN, LA> SA;
+  typedef Carry<T, TL::BN, TL::WM * TL::WN, LB> SB;
+  constexpr int BK = SA::BK;
+  constexpr int STAGE = SA::BYTES + SB::BYTES;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+  const int t = threadIdx.x, lane = t & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wm = wave % TL::WM, wn = wave / TL::WM;
+
+  const TileAt q = tile_at(g, blockIdx.x);
+  const int64_t k_begin = q.part * g.k_part;
+  const int64_t k_end = k_begin + g.k_part < g.k ? k_begin + g.k_part : g.k;
+
+  typename Mma<T>::Acc acc[TL::MI][TL::NI];
+#pragma unroll
+  for (int i = 0; i < TL::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < TL::NI; ++j) acc[i][j] = typename Mma<T>::Acc{};
+
+  SA sa;
+  SB sb;
+  sa.init(a, (int64_t)q.m * TL::BM, k_begin, k_end, wave, lane);
+  sb.init(b, (int64_t)q.n * TL::BN, k_begin, k_end, wave, lane);
+  int left = (int)(k_end - k_begin), stage = 0;
+  if (left > 0) {
+    sa.load(left);
+    sb.load(left);
+    sa.store(lds, wave, lane);
+    sb.store(lds + SA::BYTES, wave, lane);
+  }
+  meet();
+  for (; left > 0; left -= BK) {
+    if (left > BK) {
+      sa.load(left - BK);
+      sb.load(left - BK);
+    }
+    const char* const tile = lds + stage * STAGE;
+    stage ^= 1;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      u32x4 fa[TL::MI], fb[TL::NI];
+#pragma unroll
+      for (int i = 0; i < TL::MI; ++i) fa[i] = SA::fragment(tile, wm * TL::MI * 16 + i * 16, s, lane);
+#pragma unroll
+      for (int j = 0; j < TL::NI; ++j) fb[j] = SB::fragment(tile + SA::BYTES, wn * TL::NI * 16 + j * 16, s, lane);
+#pragma unroll
+      for (int p = 0; p < Mma<T>::PARTS; ++p)
+#pragma unroll
+        for (int i = 0; i < TL::MI; ++i)
+#pragma unroll
+          for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[i], fb[j], acc[i][j], p);
+    }
+    if (left > BK) {  // into the space that all have read before they last met
+      sa.store(lds + stage * STAGE, wave, lane);
+      sb.store(lds + stage * STAGE + SA::BYTES, wave, lane);
+    }
+    meet();
+  }
   e.template run<TL>(acc, place_of<TL>(q, a.rows, b.rows, wm, wn, lane, t), lds);
 }
 
@@ -662,7 +700,7 @@ struct SoftmaxShares {
       for (int d = 16; d < kWave; d *= 2) s = join(s, Share{__shfl_xor(s.top, d), __shfl_xor(s.sum, d)});
       if (w.lane < 16) red[w.wm * TL::BN + w.n(j)] = s;
     }
-    __syncthreads();
+    meet();
     for (int c = w.t; c < w.left_n; c += TL::THREADS) {
       Share s = red[c];
 #pragma unroll
@@ -883,14 +921,12 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 bool launch_fits(int64_t groups, int threads) { return groups < ((int64_t)1 << 32) / threads; }
 
-typedef Tile<64, 64, 2, 2> SimpleTile;  // operands of any alignment
-
 constexpr int64_t kMostRows = (int64_t)1 << 24;   // of hidden
 constexpr int64_t kMostWidth = (int64_t)1 << 17;  // an int32 sum of 2^17 - 1 products of codes holds
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 
-// The tiles of aligned operands, m (vocabulary or width) by n.
-enum class Shape { Simple, Large, Wide, Medium, Low, Few };
+// The tiles of a product, m (vocabulary or width) by n.
+enum class Shape { Large, Wide, Medium, Low, Few };
 struct LargeTile : Tile<256, 256, 2, 4> {  // one workgroup per compute unit
   static constexpr int STAGES = 2;
 };
@@ -906,11 +942,11 @@ struct LowTile : Tile<128, 64, 4, 2> {
 struct FewTile : Tile<64, 32, 2, 2> {
   static constexpr int STAGES = 4;
 };
-int tile_m(Shape s) { return s == Shape::Large ? 256 : s == Shape::Simple || s == Shape::Few ? 64 : 128; }
+int tile_m(Shape s) { return s == Shape::Large ? 256 : s == Shape::Few ? 64 : 128; }
 int tile_n(Shape s) {
   return s == Shape::Large ? 256 : s == Shape::Wide ? 192 : s == Shape::Medium ? 128 : s == Shape::Few ? 32 : 64;
 }
-int threads_of(Shape s) { return s == Shape::Simple || s == Shape::Few ? 256 : 512; }
+int threads_of(Shape s) { return s == Shape::Few ? 256 : 512; }
 
 // Whether a side can be read directly: rows at multiples of 16 bytes, k of a row-major side
 // in whole chunks (so a transposed one's lines are too: `along` is the width in either), and
@@ -925,6 +961,11 @@ bool direct(const Side& s, int64_t along) {
          s.stride * (int64_t)sizeof(T) < ((int64_t)1 << 31) / most;
 }
 
+// How the operands of a product come into LDS, and its tiles.
+struct Way {
+  bool direct;
+  Shape shape;
+};
 template <typename T, class TL, Load LA, Load LB, class Epilogue>
 void launch_direct(const Side& a, const Side& b, const Grid& g, unsigned groups, const Epilogue& e, hipStream_t st) {
   hipLaunchKernelGGL((k_product_direct<T, TL, false, LA, LB, Epilogue>), dim3(groups), dim3(TL::THREADS), 0, st, a, b, g,
@@ -963,9 +1004,11 @@ struct Cut {
 // 32000 x 1024 x 256).  bf16, us of large, wide and medium: 16384 x 8192 x 4096 790, 851 and
 // 962; 50257 x 2048 x 768 164, 158 and 173; 50257 x 1000 x 768 92, 94 and 92; 1024 x 4096
 // over k = 32000 684, 464 and 410, in four parts 216, 278 and 280.
-Cut cut_of(int64_t m, int64_t n, int64_t k, int es, int most_parts) {
+Cut cut_of(int64_t m, int64_t n, int64_t k, int es, int most_parts, bool direct = true) {
   const int64_t tiles_k = ceil_div(k * es, kRowBytes);
-  if (n <= 64 && most_parts <= 1) return Cut{n <= 32 ? Shape::Few : Shape::Low, 1};
+  if (n <= 32 && most_parts <= 1) return Cut{Shape::Few, 1};
+  if (!direct) return Cut{Shape::Medium, 1};
+  if (n <= 64 && most_parts <= 1) return Cut{Shape::Low, 1};
   Cut best{Shape::Medium, 1};
   double least = INFINITY;
   for (const Shape s : {Shape::Large, Shape::Wide, Shape::Medium}) {
@@ -990,8 +1033,9 @@ bool product_fits(Shape s, int64_t m, int64_t n, int parts) {
   return launch_fits(product_groups(s, m, n, parts), threads_of(s));
 }
 template <typename T, Load LA, Load LB, class Epilogue>
-void launch_product(Shape s, const Side& a, const Side& b, int64_t k, int parts, const Epilogue& e, hipStream_t st) {
-  constexpr int BK = kRowBytes / sizeof(T);  // a multiple of every tile's k
+void launch_product(Way way, const Side& a, const Side& b, int64_t k, int parts, const Epilogue& e, hipStream_t st) {
+  constexpr int BK = kRowBytes / sizeof(T);  // of every tile
+  const Shape s = way.shape;
   Grid g;
   g.tiles_m = (int32_t)ceil_div(a.rows, tile_m(s));
   g.tiles_n = (int32_t)ceil_div(b.rows, tile_n(s));
@@ -999,11 +1043,18 @@ void launch_product(Shape s, const Side& a, const Side& b, int64_t k, int parts,
   g.k_part = round_up(ceil_div(k, parts), BK);
   g.parts = parts;
   const unsigned groups = (unsigned)product_groups(s, a.rows, b.rows, parts);
-  switch (s) {
-    case Shape::Simple:
-      hipLaunchKernelGGL((k_product<T, SimpleTile, LA, LB, Epilogue>), dim3(groups), dim3(SimpleTile::THREADS), 0, st, a,
+  if (!way.direct) {  // medium or, of row-major operands, few (cut_of)
+    if (LA == Load::Rows && s == Shape::Few) {
+      if constexpr (LA == Load::Rows)
+        hipLaunchKernelGGL((k_product<T, FewTile, LA, LB, Epilogue>), dim3(groups), dim3(FewTile::THREADS), 0, st, a, b,
+                           g, e);
+    } else {
+      hipLaunchKernelGGL((k_product<T, MediumTile, LA, LB, Epilogue>), dim3(groups), dim3(MediumTile::THREADS), 0, st, a,
                          b, g, e);
-      break;
+    }
+    return;
+  }
+  switch (s) {
     case Shape::Large:  // 8 and 16 bits (cut_of)
       if constexpr (sizeof(T) < 4) launch_direct<T, LargeTile, LA, LB>(a, b, g, groups, e, st);
       break;
@@ -1069,14 +1120,15 @@ struct LossArgs {
 };
 
 size_t loss_bytes(int64_t n, int64_t vocab) {
-  return (size_t)round_up(n * ceil_div(vocab, SimpleTile::BM) * (int64_t)sizeof(Share), 256) + (size_t)round_up(n * 4, 256);
+  // by the lowest tile: the operands' alignment is not known here
+  return (size_t)round_up(n * ceil_div(vocab, FewTile::BM) * (int64_t)sizeof(Share), 256) + (size_t)round_up(n * 4, 256);
 }
 
 template <typename T>
 cmsd_status enqueue_loss(const LossArgs& a, float* loss, float* lse, void* workspace, hipStream_t st) {
   const Side w{a.weight, a.weight_stride, a.vocab, a.width}, h{a.hidden, a.hidden_stride, a.n, a.width};
   const bool fast = direct<T, Load::Rows>(w, a.width) && direct<T, Load::Rows>(h, a.width);
-  const Shape s = fast ? cut_of(a.vocab, a.n, a.width, sizeof(T), 1).shape : Shape::Simple;
+  const Shape s = cut_of(a.vocab, a.n, a.width, sizeof(T), 1, fast).shape;
   if (!product_fits(s, a.vocab, a.n, 1)) return CMSD_ERR_ARG;
   SoftmaxShares e;
   e.scale = a.scale;
@@ -1085,7 +1137,7 @@ cmsd_status enqueue_loss(const LossArgs& a, float* loss, float* lse, void* works
   e.shares = static_cast<Share*>(workspace);
   e.at_label = reinterpret_cast<float*>(static_cast<char*>(workspace) +
                                         round_up(a.n * (int64_t)e.tiles_m * (int64_t)sizeof(Share), 256));
-  launch_product<T, Load::Rows, Load::Rows>(s, w, h, a.width, 1, e, st);
+  launch_product<T, Load::Rows, Load::Rows>(Way{fast, s}, w, h, a.width, 1, e, st);
   hipLaunchKernelGGL(k_loss, dim3((unsigned)ceil_div(a.n, 4)), dim3(256), 0, st, e.shares, e.tiles_m, e.at_label,
                      a.labels, a.n, a.vocab, loss, lse);
   return launched();
@@ -1118,36 +1170,37 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
   // the workspace's rows are aligned, and so are the operands' pieces where the operands are
   const bool fast = direct<T, Load::Rows>(w0, a.width) && direct<T, Load::Rows>(h, a.width) &&
                     direct<T, Load::Columns>(w0, a.width) && direct<T, Load::Columns>(h, a.width);
-  const Shape zs = fast ? cut_of(p.piece, a.n, a.width, sizeof(T), 1).shape : Shape::Simple;
-  const Shape hshape = fast ? p.hidden.shape : Shape::Simple, wshape = fast ? p.weight.shape : Shape::Simple;
-  if (!product_fits(zs, p.piece, a.n, 1) || (grad_hidden && !product_fits(hshape, a.width, a.n, p.hidden.parts)) ||
-      (grad_weight && !product_fits(wshape, a.width, p.piece, p.weight.parts)))
+  const Way zway{fast, cut_of(p.piece, a.n, a.width, sizeof(T), 1, fast).shape};
+  const Way hway{fast, fast ? p.hidden.shape : Shape::Medium}, wway{fast, fast ? p.weight.shape : Shape::Medium};
+  if (!product_fits(zway.shape, p.piece, a.n, 1) ||
+      (grad_hidden && !product_fits(hway.shape, a.width, a.n, p.hidden.parts)) ||
+      (grad_weight && !product_fits(wway.shape, a.width, p.piece, p.weight.parts)))
     return CMSD_ERR_ARG;
   for (int64_t v = 0; v < a.vocab; v += p.piece) {
     const int64_t m = a.vocab - v < p.piece ? a.vocab - v : p.piece;
     const T* const rows = static_cast<const T*>(a.weight) + v * a.weight_stride;
     const Side w{rows, a.weight_stride, m, a.width};
     LogitGradient<T> e{a.scale, a.labels, lse, grad_loss, v, a.vocab, dz, p.stride};
-    launch_product<T, Load::Rows, Load::Rows>(zs, w, h, a.width, 1, e, st);
+    launch_product<T, Load::Rows, Load::Rows>(zway, w, h, a.width, 1, e, st);
     if (grad_hidden) {
       const int64_t k = round_up(m, kPad);
       const Side wt{rows, a.weight_stride, a.width, m}, d{dz, p.stride, a.n, k};
       if (slabs)
-        launch_product<T, Load::Columns, Load::Rows>(hshape, wt, d, k, p.hidden.parts,
+        launch_product<T, Load::Columns, Load::Rows>(hway, wt, d, k, p.hidden.parts,
                                                      Slabs{hs, a.width, a.n * a.width, v > 0}, st);
       else
-        launch_product<T, Load::Columns, Load::Rows>(hshape, wt, d, k, 1,
+        launch_product<T, Load::Columns, Load::Rows>(hway, wt, d, k, 1,
                                                      Plain<T>{static_cast<T*>(grad_hidden), gh_stride}, st);
     }
     if (grad_weight) {
       const Side dt{dz, p.stride, m, a.n};
       T* const out = static_cast<T*>(grad_weight) + v * gw_stride;
       if (p.weight.parts > 1) {
-        launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, p.weight.parts,
+        launch_product<T, Load::Columns, Load::Columns>(wway, ht, dt, a.n, p.weight.parts,
                                                         Slabs{wsl, a.width, m * a.width, false}, st);
         sum_slabs<T>(wsl, p.weight.parts, m * a.width, m, a.width, out, gw_stride, st);
       } else {
-        launch_product<T, Load::Columns, Load::Columns>(wshape, ht, dt, a.n, 1, Plain<T>{out, gw_stride}, st);
+        launch_product<T, Load::Columns, Load::Columns>(wway, ht, dt, a.n, 1, Plain<T>{out, gw_stride}, st);
       }
     }
   }
@@ -1219,15 +1272,15 @@ cmsd_status cmsd_head_logits(const int8_t* hidden, int64_t hidden_stride, const 
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Side w{weight, weight_stride, vocab, width}, h{hidden, hidden_stride, n_rows, width};
   const bool fast = direct<int8_t, Load::Rows>(w, width) && direct<int8_t, Load::Rows>(h, width);
-  const Shape s = fast ? cut_of(vocab, n_rows, width, 1, 1).shape : Shape::Simple;
-  if (!product_fits(s, vocab, n_rows, 1)) return CMSD_ERR_ARG;
+  const Way way{fast, cut_of(vocab, n_rows, width, 1, 1, fast).shape};
+  if (!product_fits(way.shape, vocab, n_rows, 1)) return CMSD_ERR_ARG;
   if (dtype == CMSD_F32)
     launch_product<int8_t, Load::Rows, Load::Rows>(
-        s, w, h, width, 1,
+        way, w, h, width, 1,
         LogitRows<float>{hidden_scales, weight_scales, scale, static_cast<float*>(logits), logit_stride}, st);
   else
     launch_product<int8_t, Load::Rows, Load::Rows>(
-        s, w, h, width, 1,
+        way, w, h, width, 1,
         LogitRows<Bf16>{hidden_scales, weight_scales, scale, static_cast<Bf16*>(logits), logit_stride}, st);
   return launched();
 }
