@@ -926,7 +926,7 @@ constexpr int64_t kMostWidth = (int64_t)1 << 17;  // an int32 sum of 2^17 - 1 pr
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 
 // The tiles of a product, m (vocabulary or width) by n.
-enum class Shape { Large, Wide, Medium, Low, Few };
+enum class Shape { Large, Wide, Medium, Low, Small, Few };
 struct LargeTile : Tile<256, 256, 2, 4> {  // one workgroup per compute unit
   static constexpr int STAGES = 2;
 };
@@ -939,10 +939,13 @@ struct MediumTile : Tile<128, 128, 2, 4> {  // two
 struct LowTile : Tile<128, 64, 4, 2> {
   static constexpr int STAGES = 3;
 };
+struct SmallTile : Tile<64, 64, 2, 4> {
+  static constexpr int STAGES = 3;
+};
 struct FewTile : Tile<64, 32, 2, 2> {
   static constexpr int STAGES = 4;
 };
-int tile_m(Shape s) { return s == Shape::Large ? 256 : s == Shape::Few ? 64 : 128; }
+int tile_m(Shape s) { return s == Shape::Large ? 256 : s == Shape::Small || s == Shape::Few ? 64 : 128; }
 int tile_n(Shape s) {
   return s == Shape::Large ? 256 : s == Shape::Wide ? 192 : s == Shape::Medium ? 128 : s == Shape::Few ? 32 : 64;
 }
@@ -959,6 +962,11 @@ bool direct(const Side& s, int64_t along) {
   const int64_t most = LOAD == Load::Columns ? 64 : s.rows < 256 ? s.rows : 256;
   return ((uintptr_t)s.p & 15) == 0 && s.stride % E == 0 && along % E == 0 &&
          s.stride * (int64_t)sizeof(T) < ((int64_t)1 << 31) / most;
+}
+
+template <typename T, class TL, Load LA, Load LB, class Epilogue>
+void launch_any(const Side& a, const Side& b, const Grid& g, unsigned groups, const Epilogue& e, hipStream_t st) {
+  hipLaunchKernelGGL((k_product<T, TL, LA, LB, Epilogue>), dim3(groups), dim3(TL::THREADS), 0, st, a, b, g, e);
 }
 
 // How the operands of a product come into LDS, and its tiles.
@@ -991,39 +999,64 @@ struct Cut {
   Shape shape;
   int parts;
 };
+// What a round of workgroups of a shape takes: us per tile of 128 bytes of k for a
+// workgroup alone on its compute unit and for as many as the chip holds (slots, on 256
+// compute units), and us for its start and end.  32 bits are bound by the matrix cores
+// whatever the tile (the large one spilled registers: 146 against 143 us for
+// 32000 x 1024 x 256).
+struct Pace {
+  Shape shape;
+  double alone, full;
+  int64_t slots;
+  double start;
+};
+constexpr Pace kPaces[] = {{Shape::Large, 1.27, 1.45, 256, 7.0},
+                           {Shape::Wide, 0.68, 1.21, 512, 3.0},
+                           {Shape::Medium, 0.57, 0.92, 512, 2.0},
+                           {Shape::Low, 0.35, 0.62, 512, 2.0},
+                           {Shape::Small, 0.25, 0.60, 768, 2.0}};
+constexpr Pace kPaces32[] = {{Shape::Medium, 1.95, 3.9, 512, 4.0},
+                             {Shape::Low, 0.98, 2.1, 512, 2.5},
+                             {Shape::Small, 0.49, 1.55, 768, 2.0}};
+// Operands through registers: a workgroup alone waits for its loads, and two fill the gaps
+// (1550 x 103477 x 2127 in 8 bits 38 us a round, 2048 x 50257 x 768 bf16 19).
+constexpr Pace kPacesAny[] = {{Shape::Medium, 1.5, 1.6, 512, 2.0}, {Shape::Small, 0.9, 1.2, 768, 2.0}};
+constexpr Pace kPacesAny32[] = {{Shape::Medium, 2.6, 4.2, 512, 4.0}, {Shape::Small, 1.1, 1.9, 768, 2.0}};
+double expected_us(const Pace& p, int64_t groups, int64_t tiles_k) {
+  const int64_t rounds = (groups - 1) / p.slots, last = groups - rounds * p.slots;
+  return rounds * (tiles_k * p.full + p.start) + tiles_k * (last <= 256 ? p.alone : p.full) + p.start;
+}
 // Few rows (n) take tiles as low as they are: such a product reads its weight once and is
 // bound by that (4 to 16 waves of a compute unit on it; 16 rows of 32000 x 4096 in bf16,
 // 262 MB, 38 us with tiles of 64 x 32, 40 with 128 x 32, 42 with 256 x 32; 64 rows
-// of 152064 x 4096 in 8 bits 128 us with 128 x 64, 153 with 128 x 128).  Else the tile and, where most_parts allows, the parts of k are those that
-// are expected to take least: rounds of workgroups over the chip, each round its tiles of
-// 128 bytes of k and a start and an end worth some more, and the slabs of parts written and
-// read.  Measured on 256 compute units, us per tile of k and round, and the start and end in
-// tiles of k: large 1.45 and 5, wide 1.21 and 2.5, medium 0.92 and 2 (two workgroups of
-// either on a compute unit); 32 bits, bound by the matrix cores whatever the tile, medium
-// 3.9 and 1 (large spilled registers and was slower, 146 against 143 us for
-// 32000 x 1024 x 256).  bf16, us of large, wide and medium: 16384 x 8192 x 4096 790, 851 and
-// 962; 50257 x 2048 x 768 164, 158 and 173; 50257 x 1000 x 768 92, 94 and 92; 1024 x 4096
-// over k = 32000 684, 464 and 410, in four parts 216, 278 and 280.
+// of 152064 x 4096 in 8 bits 128 us with 128 x 64, 153 with 128 x 128).  Else the tile and,
+// where most_parts allows, the parts of k are those that are expected to take least, the
+// slabs of parts written and read included.  bf16, us measured of large, wide, medium, low
+// and small tiles: 16384 x 8192 x 4096 790, 851, 962; 50257 x 2048 x 768 164, 158, 173;
+// 50257 x 1000 x 768 92, 94, 92; 2000 x 2000 x 1024 30, 16, 13, 14, 17; 1674 x 462 x 3648
+// 76, 44, 39, 21, 16; 1024 x 4096 over k = 32000 684, 464, 410, in four parts 216, 278, 280.
+// Products with parts have transposed operands and tiles of 128 or more.
 Cut cut_of(int64_t m, int64_t n, int64_t k, int es, int most_parts, bool direct = true) {
   const int64_t tiles_k = ceil_div(k * es, kRowBytes);
-  if (n <= 32 && most_parts <= 1) return Cut{Shape::Few, 1};
-  if (!direct) return Cut{Shape::Medium, 1};
-  if (n <= 64 && most_parts <= 1) return Cut{Shape::Low, 1};
+  const bool rows = most_parts <= 1;
+  if (n <= 32 && rows) return Cut{Shape::Few, 1};
+  if (n <= 64 && rows && ceil_div(m, 128) >= 160 && direct) return Cut{Shape::Low, 1};
   Cut best{Shape::Medium, 1};
   double least = INFINITY;
-  for (const Shape s : {Shape::Large, Shape::Wide, Shape::Medium}) {
-    if (es == 4 && s != Shape::Medium) continue;
-    const double unit = es == 4 ? 3.9 : s == Shape::Large ? 1.45 : s == Shape::Wide ? 1.21 : 0.92;
-    const double more = es == 4 ? 1.0 : s == Shape::Large ? 5.0 : s == Shape::Wide ? 2.5 : 2.0;
-    const int64_t tiles = product_groups(s, m, n, 1), slots = s == Shape::Large ? 256 : 512;
+  const Pace* const paces = direct ? (es == 4 ? kPaces32 : kPaces) : (es == 4 ? kPacesAny32 : kPacesAny);
+  const int count = direct ? (es == 4 ? 3 : 5) : 2;
+  for (int i = 0; i < count; ++i) {
+    const Pace& p = paces[i];
+    if (!rows && (p.shape == Shape::Low || p.shape == Shape::Small)) continue;
+    const int64_t tiles = product_groups(p.shape, m, n, 1);
     for (int parts = 1; parts <= most_parts && (parts == 1 || tiles_k / parts >= 4); ++parts) {
       if (ceil_div(tiles_k, ceil_div(tiles_k, parts)) < parts) continue;  // a part would be empty
       const double slabs = parts > 1 ? 2.0 * parts * m * n * 4 / 4e6 : 0.0;
       if (slabs > 250.0) break;
-      const double us = ceil_div(tiles * parts, slots) * (ceil_div(tiles_k, parts) + more) * unit + slabs;
+      const double us = expected_us(p, tiles * parts, ceil_div(tiles_k, parts)) + slabs;
       if (us < least) {
         least = us;
-        best = Cut{s, parts};
+        best = Cut{p.shape, parts};
       }
     }
   }
@@ -1043,14 +1076,13 @@ void launch_product(Way way, const Side& a, const Side& b, int64_t k, int parts,
   g.k_part = round_up(ceil_div(k, parts), BK);
   g.parts = parts;
   const unsigned groups = (unsigned)product_groups(s, a.rows, b.rows, parts);
-  if (!way.direct) {  // medium or, of row-major operands, few (cut_of)
-    if (LA == Load::Rows && s == Shape::Few) {
-      if constexpr (LA == Load::Rows)
-        hipLaunchKernelGGL((k_product<T, FewTile, LA, LB, Epilogue>), dim3(groups), dim3(FewTile::THREADS), 0, st, a, b,
-                           g, e);
+  if (!way.direct) {  // medium or, of row-major operands, small or few (cut_of)
+    if (s == Shape::Few) {
+      if constexpr (LA == Load::Rows) launch_any<T, FewTile, LA, LB>(a, b, g, groups, e, st);
+    } else if (s == Shape::Small) {
+      if constexpr (LA == Load::Rows) launch_any<T, SmallTile, LA, LB>(a, b, g, groups, e, st);
     } else {
-      hipLaunchKernelGGL((k_product<T, MediumTile, LA, LB, Epilogue>), dim3(groups), dim3(MediumTile::THREADS), 0, st, a,
-                         b, g, e);
+      launch_any<T, MediumTile, LA, LB>(a, b, g, groups, e, st);
     }
     return;
   }
@@ -1064,6 +1096,9 @@ void launch_product(Way way, const Side& a, const Side& b, int64_t k, int parts,
     case Shape::Medium: launch_direct<T, MediumTile, LA, LB>(a, b, g, groups, e, st); break;
     case Shape::Low:  // row-major operands (cut_of)
       if constexpr (LA == Load::Rows) launch_few<T, LowTile, LA, LB>(a, b, g, groups, e, st);
+      break;
+    case Shape::Small:
+      if constexpr (LA == Load::Rows) launch_direct<T, SmallTile, LA, LB>(a, b, g, groups, e, st);
       break;
     case Shape::Few:
       if constexpr (LA == Load::Rows) launch_few<T, FewTile, LA, LB>(a, b, g, groups, e, st);
@@ -1084,7 +1119,7 @@ bool finite(float x) { return x - x == 0.f; }
 // rows (into the weight's).
 struct GradPlan {
   int64_t piece, stride;  // vocabulary entries of a piece; a row of its gradients
-  Cut hidden, weight;     // the two products that take them
+  Cut hidden[2], weight[2];  // the two products that take them: operands of any alignment, aligned ones
   size_t logits_at, hidden_at, weight_at, bytes;
 };
 constexpr int64_t kPieceBytes = (int64_t)1 << 28;  // of a piece's logit gradients
@@ -1096,15 +1131,20 @@ GradPlan grad_plan(int64_t n, int64_t vocab, int64_t width, int es) {
   if (p.piece > kMostPiece) p.piece = kMostPiece;
   if (p.piece > vocab) p.piece = vocab;
   p.stride = round_up(p.piece, 128);
-  p.hidden = cut_of(width, n, p.piece, es, 64);
-  p.weight = cut_of(width, p.piece, n, es, 64);
+  int hidden_parts = 1, weight_parts = 1;  // the most of either
+  for (int direct = 0; direct < 2; ++direct) {
+    p.hidden[direct] = cut_of(width, n, p.piece, es, 64, direct);
+    p.weight[direct] = cut_of(width, p.piece, n, es, 64, direct);
+    if (p.hidden[direct].parts > hidden_parts) hidden_parts = p.hidden[direct].parts;
+    if (p.weight[direct].parts > weight_parts) weight_parts = p.weight[direct].parts;
+  }
   size_t at = 0;
   p.logits_at = at;
   at += (size_t)round_up(n * p.stride * es, 256);
   p.hidden_at = at;
-  if (p.hidden.parts > 1 || p.piece < vocab) at += (size_t)round_up(p.hidden.parts * n * width * 4, 256);
+  if (hidden_parts > 1 || p.piece < vocab) at += (size_t)round_up(hidden_parts * n * width * 4, 256);
   p.weight_at = at;
-  if (p.weight.parts > 1) at += (size_t)round_up(p.weight.parts * p.piece * width * 4, 256);
+  if (weight_parts > 1) at += (size_t)round_up(weight_parts * p.piece * width * 4, 256);
   p.bytes = at;
   return p;
 }
@@ -1164,17 +1204,18 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
   T* const dz = reinterpret_cast<T*>(ws + p.logits_at);
   float* const hs = reinterpret_cast<float*>(ws + p.hidden_at);
   float* const wsl = reinterpret_cast<float*>(ws + p.weight_at);
-  const bool slabs = p.hidden.parts > 1 || p.piece < a.vocab;
   const Side h{a.hidden, a.hidden_stride, a.n, a.width}, ht{a.hidden, a.hidden_stride, a.width, a.n};
   const Side w0{a.weight, a.weight_stride, a.vocab, a.width};
   // the workspace's rows are aligned, and so are the operands' pieces where the operands are
   const bool fast = direct<T, Load::Rows>(w0, a.width) && direct<T, Load::Rows>(h, a.width) &&
                     direct<T, Load::Columns>(w0, a.width) && direct<T, Load::Columns>(h, a.width);
   const Way zway{fast, cut_of(p.piece, a.n, a.width, sizeof(T), 1, fast).shape};
-  const Way hway{fast, fast ? p.hidden.shape : Shape::Medium}, wway{fast, fast ? p.weight.shape : Shape::Medium};
+  const Cut hidden = p.hidden[fast], weight = p.weight[fast];
+  const Way hway{fast, hidden.shape}, wway{fast, weight.shape};
+  const bool slabs = hidden.parts > 1 || p.piece < a.vocab;
   if (!product_fits(zway.shape, p.piece, a.n, 1) ||
-      (grad_hidden && !product_fits(hway.shape, a.width, a.n, p.hidden.parts)) ||
-      (grad_weight && !product_fits(wway.shape, a.width, p.piece, p.weight.parts)))
+      (grad_hidden && !product_fits(hway.shape, a.width, a.n, hidden.parts)) ||
+      (grad_weight && !product_fits(wway.shape, a.width, p.piece, weight.parts)))
     return CMSD_ERR_ARG;
   for (int64_t v = 0; v < a.vocab; v += p.piece) {
     const int64_t m = a.vocab - v < p.piece ? a.vocab - v : p.piece;
@@ -1186,7 +1227,7 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
       const int64_t k = round_up(m, kPad);
       const Side wt{rows, a.weight_stride, a.width, m}, d{dz, p.stride, a.n, k};
       if (slabs)
-        launch_product<T, Load::Columns, Load::Rows>(hway, wt, d, k, p.hidden.parts,
+        launch_product<T, Load::Columns, Load::Rows>(hway, wt, d, k, hidden.parts,
                                                      Slabs{hs, a.width, a.n * a.width, v > 0}, st);
       else
         launch_product<T, Load::Columns, Load::Rows>(hway, wt, d, k, 1,
@@ -1195,17 +1236,17 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
     if (grad_weight) {
       const Side dt{dz, p.stride, m, a.n};
       T* const out = static_cast<T*>(grad_weight) + v * gw_stride;
-      if (p.weight.parts > 1) {
-        launch_product<T, Load::Columns, Load::Columns>(wway, ht, dt, a.n, p.weight.parts,
+      if (weight.parts > 1) {
+        launch_product<T, Load::Columns, Load::Columns>(wway, ht, dt, a.n, weight.parts,
                                                         Slabs{wsl, a.width, m * a.width, false}, st);
-        sum_slabs<T>(wsl, p.weight.parts, m * a.width, m, a.width, out, gw_stride, st);
+        sum_slabs<T>(wsl, weight.parts, m * a.width, m, a.width, out, gw_stride, st);
       } else {
         launch_product<T, Load::Columns, Load::Columns>(wway, ht, dt, a.n, 1, Plain<T>{out, gw_stride}, st);
       }
     }
   }
   if (grad_hidden && slabs)
-    sum_slabs<T>(hs, p.hidden.parts, a.n * a.width, a.n, a.width, grad_hidden, gh_stride, st);
+    sum_slabs<T>(hs, hidden.parts, a.n * a.width, a.n, a.width, grad_hidden, gh_stride, st);
   return launched();
 }
 

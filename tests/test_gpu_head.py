@@ -276,7 +276,8 @@ def _on_gpu(h, wt, y, gl, scale, dtype):
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n,v,w,pad", [(700, 17000, 64, 0), (3300, 600, 4096, 0), (300, 13000, 1024, 8),
                                        (4100, 13001, 264, 0), (1024, 50257, 8, 0), (32, 50000, 136, 0),
-                                       (50, 30001, 520, 8)])
+                                       (50, 30001, 520, 8), (400, 2000, 1000, 0), (60, 4001, 320, 0),
+                                       (90, 15000, 136, 3), (260, 9000, 129, 0)])
 def test_every_tile_of_the_products(cm, dtype, n, v, w, pad):
     # extents that take the largest tiles in one product or another, and ragged ones in all
     h, wt, y, _, _, _, gl = problem(n, n, v, w, dtype, pad)
