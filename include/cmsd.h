@@ -454,6 +454,7 @@ size_t cmsd_draft_sample_workspace_bytes(int64_t n_rows, int64_t vocab);
 /*
  * The vocabulary projection ("head") around the logit pass: the product that makes logit
  * rows, in 8-bit integers, and the loss that a drafter's head (or its trunk) is fitted with.
+ * No output of these calls may overlap an input or the workspace.
  *
  * cmsd_quantize_rows - rows to 8-bit codes with one scale each: scale = max|x| / 127 in
  * single precision, code = the whole number next to x / scale, ties to even.  Quantises
@@ -531,8 +532,10 @@ size_t cmsd_head_loss_workspace_bytes(int64_t n_rows, int64_t vocab);
  *   d[n][v] = grad_loss[n] * scale * (exp(z[n][v] - lse[n]) - [v = labels[n]])
  *   grad_hidden = d . weight,  grad_weight = d^T . hidden.
  * The vocabulary is taken in pieces: a piece's logits are formed again and only its d is
- * held, rounded to dtype as the products take it; the products are summed in single
- * precision and rounded once.  Rows with a negative label, or one >= vocab, add nothing.
+ * held, over the largest |grad_loss * scale| and rounded to dtype as the products take it;
+ * the products are summed in single precision and rounded once.  Rows with a negative label,
+ * one >= vocab or a grad_loss of 0 add nothing, whatever they hold (NaN and infinities in
+ * padding among it); their own gradients are zeros under a finite weight.
  *
  *   hidden .. width  as for cmsd_head_loss.  n_rows = 0 fills grad_weight with zeros.
  *   lse, grad_loss   device, n_rows floats each.

@@ -538,9 +538,9 @@ __global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g,
 // contiguous run: stored from the accumulators, eight bytes of sixteen rows at a time, a
 // tile of 256 x 256 took a tenth of the time of its products over k = 4096.  LAST: nothing
 // of the call reads them again, and the stores are marked so, which leaves the operands in
-// the caches (256 x 128256 x 2048 in 8 bits 82 -> 73 us, 576 x 50257 x 768 47 -> 40).  (The vectors may
-// start at any element: the memory pipeline takes that.)  A wave's LDS operations are done
-// in their order.  add: to what is there.
+// the caches (256 x 128256 x 2048 in 8 bits 82 -> 73 us, 576 x 50257 x 768 47 -> 40).  (The
+// vectors may start at any element: the memory pipeline takes that.)  A wave's LDS
+// operations are done in their order.  add: to what is there.
 template <bool LAST, typename T, class TL, class F>
 __device__ __forceinline__ void store_rows(const Place<TL>& w, char* lds, T* out, int64_t stride, int left_m, bool add,
                                            const F& value) {
@@ -710,22 +710,34 @@ struct SoftmaxShares {
   }
 };
 
-// The gradient by the logits, g * scale * (softmax - [v = label]), of a piece of the
-// vocabulary, rounded to the type of the products that take it.  Rows end in zeros up to a
-// whole chunk: k of the product that takes them along their length.
+// What a row's gradient is multiplied with: nothing but zeros come of a row without a loss,
+// or with one that does not count.
+__device__ __forceinline__ float row_factor(int64_t label, int64_t vocab, float grad_loss, float scale) {
+  return label >= 0 && label < vocab ? grad_loss * scale : 0.f;
+}
+
+// The gradient by the logits, factor * (softmax - [v = label]), of a piece of the
+// vocabulary, rounded to the type of the products that take it.  The rows' factors are taken
+// over the largest, which the products' sums are multiplied with: where all are alike (a mean
+// over the rows), a label's entry is nearly -1, which rounding leaves alone; with the factor
+// in it, every row's largest entry was off by the same part of itself (up to 2^-8: bf16,
+// 1000 rows of 50257 x 768, both gradients' distance from the exact ones 0.0029 of their
+// norm, of which their own rounding is 0.0017).  Rows end in zeros up to a whole chunk: k of
+// the product that takes them along their length.
 template <typename T>
 struct LogitGradient {
   float scale;
   const int32_t* labels;
   const float* lse;
   const float* grad_loss;
+  const float* top;  // the largest factor's magnitude
   int64_t first, vocab;  // the piece's first entry; entries in all
   T* out;
   int64_t stride;
 
   template <class TL, class Acc>
   __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, char* lds) const {
-    const float mul = scale * kLog2e;
+    const float mul = scale * kLog2e, most = *top;
     float less[TL::NI], g[TL::NI];
     int at[TL::NI];
     bool counts[TL::NI];
@@ -733,8 +745,9 @@ struct LogitGradient {
     for (int j = 0; j < TL::NI; ++j) {
       const int64_t n = w.n0 + (w.n(j) < w.left_n ? w.n(j) : 0);
       const int64_t label = labels[n];
-      counts[j] = label >= 0 && label < vocab;
-      g[j] = grad_loss[n] * scale;
+      g[j] = row_factor(label, vocab, grad_loss[n], scale);
+      counts[j] = g[j] != 0.f;
+      g[j] = most > 0.f ? g[j] / most : g[j];
       less[j] = -lse[n] * kLog2e;
       at[j] = near(label - first, w);
     }
@@ -755,15 +768,17 @@ struct LogitGradient {
   }
 };
 
-// A product as it is, rounded to T.
+// A product times *factor, rounded to T.
 template <typename T>
 struct Plain {
   T* out;
   int64_t stride;
+  const float* factor;
 
   template <class TL, class Acc>
   __device__ __forceinline__ void run(Acc& acc, const Place<TL>& w, char* lds) const {
-    store_rows<true>(w, lds, out, stride, w.left_m, false, [&](int i, int j, int r) { return acc[i][j][r]; });
+    const float f = *factor;
+    store_rows<true>(w, lds, out, stride, w.left_m, false, [&](int i, int j, int r) { return acc[i][j][r] * f; });
   }
 };
 
@@ -805,14 +820,15 @@ __global__ __launch_bounds__(256) void k_loss(const Share* shares, int32_t tiles
   }
 }
 
-// The slabs of a product summed, in their order, into rows of T.
+// The slabs of a product summed, in their order, times *factor into rows of T.
 template <typename T>
 __global__ __launch_bounds__(256) void k_sum_slabs(const float* slabs, int32_t parts, int64_t slab, int64_t rows,
-                                                   int64_t width, T* out, int64_t stride) {
+                                                   int64_t width, const float* factor, T* out, int64_t stride) {
+  const float f = *factor;
   for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < rows * width; at += (int64_t)gridDim.x * 256) {
     float x = slabs[at];
     for (int p = 1; p < parts; ++p) x += slabs[p * slab + at];
-    out[at / width * stride + at % width] = from_float<T>(x);
+    out[at / width * stride + at % width] = from_float<T>(x * f);
   }
 }
 
@@ -820,6 +836,45 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_zero_rows(T* out, int64_t rows, int64_t width, int64_t stride) {
   for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < rows * width; at += (int64_t)gridDim.x * 256)
     out[at / width * stride + at % width] = from_float<T>(0.f);
+}
+
+// What the gradient's products need beside the operands.  Workgroup 0: the largest magnitude
+// of the rows' finite factors.  The others: the rows that count, at stride round_up(width,
+// kPad) and aligned, zeros in the place of the rest: their gradients by the logits are zeros,
+// but zero times what padding may hold (NaN, infinities) is not.  (The weight's gradient so
+// takes its operands' lines whole and aligned, whatever the caller's are.)
+constexpr int kPrepare = 1024;  // threads
+template <typename T>
+__global__ __launch_bounds__(kPrepare) void k_prepare(const T* hidden, int64_t stride, const int32_t* labels,
+                                                      const float* grad_loss, float scale, int64_t n, int64_t vocab,
+                                                      int64_t width, float* top, T* out, int64_t chunks) {
+  constexpr int E = 16 / (int)sizeof(T);
+  __shared__ float tops[kPrepare / kWave];
+  if (blockIdx.x == 0) {
+    float most = 0.f;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < n; i += kPrepare) {
+      const float f = fabsf(row_factor(labels[i], vocab, grad_loss[i], scale));
+      most = f < INFINITY ? fmaxf(most, f) : most;
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int i = 1; i < kPrepare / kWave; ++i) most = fmaxf(most, tops[i]);
+      *top = most;
+    }
+    return;
+  }
+  const int64_t all = n * chunks, step = (int64_t)(gridDim.x - 1) * kPrepare;
+  for (int64_t at = (int64_t)(blockIdx.x - 1) * kPrepare + threadIdx.x; at < all; at += step) {
+    const int64_t row = at / chunks, first = at % chunks * E;
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (row_factor(labels[row], vocab, grad_loss[row], scale) != 0.f)
+      v = row_chunk<T>(hidden + row * stride + first, width - first);
+    *reinterpret_cast<u32x4*>(out + at * E) = v;
+  }
 }
 
 // The whole number next to x / s, ties to even, for |x| <= 127.5 s: an estimate that is off by
@@ -985,7 +1040,7 @@ void launch_direct(const Side& a, const Side& b, const Grid& g, unsigned groups,
 // again the same 128256 x 2048 (263 MB) 38 and 42.
 template <typename T, class TL, Load LA, Load LB, class Epilogue>
 void launch_few(const Side& a, const Side& b, const Grid& g, unsigned groups, const Epilogue& e, hipStream_t st) {
-  if (a.rows * g.k * (int64_t)sizeof(T) > (int64_t)384 << 20)
+  if (b.rows <= TL::BN && a.rows * g.k * (int64_t)sizeof(T) > (int64_t)384 << 20)
     hipLaunchKernelGGL((k_product_direct<T, TL, true, LA, LB, Epilogue>), dim3(groups), dim3(TL::THREADS), 0, st, a, b, g,
                        e);
   else
@@ -1076,12 +1131,12 @@ void launch_product(Way way, const Side& a, const Side& b, int64_t k, int parts,
   g.k_part = round_up(ceil_div(k, parts), BK);
   g.parts = parts;
   const unsigned groups = (unsigned)product_groups(s, a.rows, b.rows, parts);
-  if (!way.direct) {  // medium or, of row-major operands, small or few (cut_of)
+  if (!way.direct) {  // medium or, of row-major operands, small or few (cut_of); b row-major
     if (s == Shape::Few) {
       if constexpr (LA == Load::Rows) launch_any<T, FewTile, LA, LB>(a, b, g, groups, e, st);
     } else if (s == Shape::Small) {
       if constexpr (LA == Load::Rows) launch_any<T, SmallTile, LA, LB>(a, b, g, groups, e, st);
-    } else {
+    } else if constexpr (LB == Load::Rows) {
       launch_any<T, MediumTile, LA, LB>(a, b, g, groups, e, st);
     }
     return;
@@ -1119,8 +1174,9 @@ bool finite(float x) { return x - x == 0.f; }
 // rows (into the weight's).
 struct GradPlan {
   int64_t piece, stride;  // vocabulary entries of a piece; a row of its gradients
-  Cut hidden[2], weight[2];  // the two products that take them: operands of any alignment, aligned ones
-  size_t logits_at, hidden_at, weight_at, bytes;
+  Cut hidden[2], weight;  // the two products that take them (the weight's rows of any alignment, aligned)
+  int64_t rows_stride;    // of the hidden rows that count (k_prepare)
+  size_t logits_at, top_at, rows_at, hidden_at, weight_at, bytes;
 };
 constexpr int64_t kPieceBytes = (int64_t)1 << 28;  // of a piece's logit gradients
 constexpr int64_t kMostPiece = (int64_t)1 << 20;   // entries: 64 of its rows keep their offsets in 31 bits
@@ -1131,16 +1187,18 @@ GradPlan grad_plan(int64_t n, int64_t vocab, int64_t width, int es) {
   if (p.piece > kMostPiece) p.piece = kMostPiece;
   if (p.piece > vocab) p.piece = vocab;
   p.stride = round_up(p.piece, 128);
-  int hidden_parts = 1, weight_parts = 1;  // the most of either
-  for (int direct = 0; direct < 2; ++direct) {
-    p.hidden[direct] = cut_of(width, n, p.piece, es, 64, direct);
-    p.weight[direct] = cut_of(width, p.piece, n, es, 64, direct);
-    if (p.hidden[direct].parts > hidden_parts) hidden_parts = p.hidden[direct].parts;
-    if (p.weight[direct].parts > weight_parts) weight_parts = p.weight[direct].parts;
-  }
+  p.rows_stride = round_up(width, kPad);
+  for (int direct = 0; direct < 2; ++direct) p.hidden[direct] = cut_of(width, n, p.piece, es, 64, direct);
+  p.weight = cut_of(width, p.piece, n, es, 64);
+  const int hidden_parts = p.hidden[0].parts > p.hidden[1].parts ? p.hidden[0].parts : p.hidden[1].parts;
+  const int weight_parts = p.weight.parts;
   size_t at = 0;
   p.logits_at = at;
   at += (size_t)round_up(n * p.stride * es, 256);
+  p.top_at = at;
+  at += 256;
+  p.rows_at = at;
+  at += (size_t)round_up(n * p.rows_stride * es, 256);
   p.hidden_at = at;
   if (hidden_parts > 1 || p.piece < vocab) at += (size_t)round_up(hidden_parts * n * width * 4, 256);
   p.weight_at = at;
@@ -1190,10 +1248,10 @@ unsigned element_groups(int64_t elements) {
 }
 
 template <typename T>
-void sum_slabs(const float* slabs, int parts, int64_t slab, int64_t rows, int64_t width, void* out, int64_t stride,
-               hipStream_t st) {
+void sum_slabs(const float* slabs, int parts, int64_t slab, int64_t rows, int64_t width, const float* factor, void* out,
+               int64_t stride, hipStream_t st) {
   hipLaunchKernelGGL(k_sum_slabs<T>, dim3(element_groups(rows * width)), dim3(256), 0, st, slabs, parts, slab, rows,
-                     width, static_cast<T*>(out), stride);
+                     width, factor, static_cast<T*>(out), stride);
 }
 
 template <typename T>
@@ -1202,26 +1260,32 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
   const GradPlan p = grad_plan(a.n, a.vocab, a.width, sizeof(T));
   char* const ws = static_cast<char*>(workspace);
   T* const dz = reinterpret_cast<T*>(ws + p.logits_at);
+  float* const top = reinterpret_cast<float*>(ws + p.top_at);
+  T* const counted = reinterpret_cast<T*>(ws + p.rows_at);
   float* const hs = reinterpret_cast<float*>(ws + p.hidden_at);
   float* const wsl = reinterpret_cast<float*>(ws + p.weight_at);
-  const Side h{a.hidden, a.hidden_stride, a.n, a.width}, ht{a.hidden, a.hidden_stride, a.width, a.n};
+  const Side h{a.hidden, a.hidden_stride, a.n, a.width}, ht{counted, p.rows_stride, a.width, a.n};
   const Side w0{a.weight, a.weight_stride, a.vocab, a.width};
-  // the workspace's rows are aligned, and so are the operands' pieces where the operands are
-  const bool fast = direct<T, Load::Rows>(w0, a.width) && direct<T, Load::Rows>(h, a.width) &&
-                    direct<T, Load::Columns>(w0, a.width) && direct<T, Load::Columns>(h, a.width);
-  const Way zway{fast, cut_of(p.piece, a.n, a.width, sizeof(T), 1, fast).shape};
-  const Cut hidden = p.hidden[fast], weight = p.weight[fast];
-  const Way hway{fast, hidden.shape}, wway{fast, weight.shape};
+  // the workspace's rows are aligned, and so are the weight's pieces where the weight is
+  const bool zfast = direct<T, Load::Rows>(w0, a.width) && direct<T, Load::Rows>(h, a.width);
+  const bool hfast = direct<T, Load::Columns>(w0, a.width);
+  const Way zway{zfast, cut_of(p.piece, a.n, a.width, sizeof(T), 1, zfast).shape};
+  const Cut hidden = p.hidden[hfast], weight = p.weight;
+  const Way hway{hfast, hidden.shape}, wway{true, weight.shape};
   const bool slabs = hidden.parts > 1 || p.piece < a.vocab;
   if (!product_fits(zway.shape, p.piece, a.n, 1) ||
       (grad_hidden && !product_fits(hway.shape, a.width, a.n, hidden.parts)) ||
       (grad_weight && !product_fits(wway.shape, a.width, p.piece, weight.parts)))
     return CMSD_ERR_ARG;
+  const int64_t chunks = p.rows_stride * (int64_t)sizeof(T) / 16, copies = ceil_div(a.n * chunks, kPrepare);
+  hipLaunchKernelGGL(k_prepare<T>, dim3(grad_weight ? (unsigned)(copies < 8192 ? copies : 8192) + 1 : 1), dim3(kPrepare), 0,
+                     st, static_cast<const T*>(a.hidden), a.hidden_stride, a.labels, grad_loss, a.scale, a.n, a.vocab,
+                     a.width, top, counted, chunks);
   for (int64_t v = 0; v < a.vocab; v += p.piece) {
     const int64_t m = a.vocab - v < p.piece ? a.vocab - v : p.piece;
     const T* const rows = static_cast<const T*>(a.weight) + v * a.weight_stride;
     const Side w{rows, a.weight_stride, m, a.width};
-    LogitGradient<T> e{a.scale, a.labels, lse, grad_loss, v, a.vocab, dz, p.stride};
+    LogitGradient<T> e{a.scale, a.labels, lse, grad_loss, top, v, a.vocab, dz, p.stride};
     launch_product<T, Load::Rows, Load::Rows>(zway, w, h, a.width, 1, e, st);
     if (grad_hidden) {
       const int64_t k = round_up(m, kPad);
@@ -1231,7 +1295,7 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
                                                      Slabs{hs, a.width, a.n * a.width, v > 0}, st);
       else
         launch_product<T, Load::Columns, Load::Rows>(hway, wt, d, k, 1,
-                                                     Plain<T>{static_cast<T*>(grad_hidden), gh_stride}, st);
+                                                     Plain<T>{static_cast<T*>(grad_hidden), gh_stride, top}, st);
     }
     if (grad_weight) {
       const Side dt{dz, p.stride, m, a.n};
@@ -1239,14 +1303,14 @@ cmsd_status enqueue_grad(const LossArgs& a, const float* lse, const float* grad_
       if (weight.parts > 1) {
         launch_product<T, Load::Columns, Load::Columns>(wway, ht, dt, a.n, weight.parts,
                                                         Slabs{wsl, a.width, m * a.width, false}, st);
-        sum_slabs<T>(wsl, weight.parts, m * a.width, m, a.width, out, gw_stride, st);
+        sum_slabs<T>(wsl, weight.parts, m * a.width, m, a.width, top, out, gw_stride, st);
       } else {
-        launch_product<T, Load::Columns, Load::Columns>(wway, ht, dt, a.n, 1, Plain<T>{out, gw_stride}, st);
+        launch_product<T, Load::Columns, Load::Columns>(wway, ht, dt, a.n, 1, Plain<T>{out, gw_stride, top}, st);
       }
     }
   }
   if (grad_hidden && slabs)
-    sum_slabs<T>(hs, hidden.parts, a.n * a.width, a.n, a.width, grad_hidden, gh_stride, st);
+    sum_slabs<T>(hs, hidden.parts, a.n * a.width, a.n, a.width, top, grad_hidden, gh_stride, st);
   return launched();
 }
 

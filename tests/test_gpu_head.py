@@ -357,6 +357,64 @@ def test_rows_without_labels_and_zero_weights(cm, dtype):
     assert torch.isfinite(gh).all() and not gh[7].any() and gh[8].any() and not gh[5].any()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,v,w,pad,offset", [(70, 300, 64, 0, 0), (300, 1000, 257, 3, 1), (1000, 9000, 136, 0, 0),
+                                              (5, 40, 7, 0, 0)])
+def test_padding_that_is_not_finite(cm, dtype, n, v, w, pad, offset):
+    # what rows without a loss hold reaches neither gradient: the same bits as zeros there
+    h, wt, y, _, _, _, gl = problem(13, n, v, w, dtype, pad, offset)
+    gl = torch.from_numpy(gl).to(DEV)
+    y[1], y[2], y[n - 1], gl[3] = -1, v, -5, 0.0
+    gone = (y < 0) | (y >= v) | (gl == 0)
+    got = []
+    for fill in ((0.0, 0.0), (float("nan"), float("inf"))):
+        h[gone] = fill[0]
+        h[n - 1] = fill[1]
+        loss, lse = cm.cmsd_head_loss(h, wt, y)
+        gh, gw = torch.empty_like(h), torch.empty_like(wt)
+        cm.cmsd_head_loss_grad(h, wt, y, lse, gl, gh, gw)
+        got.append((loss[~gone], gh, gw))
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+    assert not got[1][1][gone].any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,v,w", [(900, 5000, 96), (200, 700, 65)])
+def test_a_mean_over_the_rows_is_not_biased(cm, dtype, n, v, w):
+    # one factor for all rows, 1 / n, and logits near zero: p = 1 / v, and a label's entry
+    # 1 - p is off by half a step of [1/2, 1) (UNIT / 2) at most, or is 1; the others are a
+    # 1 / v of it.  So a gradient's part along the exact one is off by UNIT / 2 + (its own
+    # rounding, of mixed signs: under UNIT / 4 of it) and the sums' (70 + v) E
+    h, wt, y, hh, ww, yy, _ = problem(17, n, v, w, dtype, scale=1e3, lean=0.0)
+    gl = np.full(n, 1 / n, np.float32)
+    _, lse = cm.cmsd_head_loss(h, wt, y, scale=1e-3)
+    gh, gw = torch.empty_like(h), torch.empty_like(wt)
+    cm.cmsd_head_loss_grad(h, wt, y, lse, torch.from_numpy(gl).to(DEV), gh, gw, scale=1e-3)
+    rh, _, rw, _, _, _ = H.head_loss_grad(hh, ww, yy, gl.astype(np.float64), 1e-3)
+    for got, ref in ((host(gh), rh), (host(gw), rw)):
+        along = (got * ref).sum() / (ref * ref).sum() - 1
+        assert abs(along) <= UNIT[dtype] * 0.75 + (70 + v) * E, along
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_factors_that_are_not_finite_stay_in_their_rows(cm, dtype):
+    h, wt, y, hh, ww, yy, gl = problem(19, 40, 300, 64, dtype)
+    y[:] = torch.arange(40, device=DEV) * 7
+    gl[4], gl[9] = np.inf, np.nan
+    _, lse = cm.cmsd_head_loss(h, wt, y)
+    gh = torch.empty_like(h)
+    cm.cmsd_head_loss_grad(h, wt, y, lse, torch.from_numpy(gl).to(DEV), grad_hidden=gh)
+    rest = [i for i in range(40) if i not in (4, 9)]
+    (rh, bh), _ = grad_bounds(hh[rest], ww, y.cpu().numpy()[rest], gl[rest].astype(np.float64), 1.0, dtype, 64)
+    within(host(gh)[rest], rh, bh, "grad_hidden")
+    assert not torch.isfinite(gh[[4, 9]]).any()
+    # none at all: zeros
+    gw = torch.empty_like(wt)
+    cm.cmsd_head_loss_grad(h, wt, y, lse, torch.zeros(40, device=DEV), gh, gw)
+    assert not gh.any() and not gw.any()
+
+
 # ------------------------------------------------------------------------------- how they are called
 def _all(cm, h, wt, y, gl, out, ws):
     cm.cmsd_quantize_rows(h, out["c"], out["s"])
