@@ -505,7 +505,8 @@ cmsd_status cmsd_head_logits(const int8_t* hidden, int64_t hidden_stride, const 
  *   lse[n] = ln sum_v exp z[n][v],  loss[n] = lse[n] - z[n][labels[n]].
  *
  *   hidden      device, n_rows rows of `width` values; weight: device, vocab rows.  Both of
- *               dtype CMSD_F32 or CMSD_BF16; sums are held in single precision.
+ *               dtype CMSD_F32 or CMSD_BF16; sums are held in single precision.  A logit
+ *               that an infinity or a NaN enters is not finite, and NaN as a rule.
  *   labels      device, n_rows int32.  A negative label has no loss (loss 0, lse as ever);
  *               a label >= vocab is an error that the row reports: its loss is NaN.
  *   scale       finite.

@@ -59,6 +59,14 @@ struct Mma<Bf16> {
   }
 };
 template <>
+struct Mma<int8_t> {
+  typedef i32x4 Acc;
+  static constexpr int PARTS = 1;
+  static __device__ __forceinline__ Acc mma(u32x4 a, u32x4 b, Acc c, int) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+  }
+};
+template <>
 struct Mma<float> {
   typedef f32x4 Acc;
   static constexpr int PARTS = 4;  // a lane's four values stand at k = 4g..4g+3 on both sides; part p takes the p-th
@@ -67,14 +75,55 @@ struct Mma<float> {
                                                 0);
   }
 };
-template <>
-struct Mma<int8_t> {
-  typedef i32x4 Acc;
-  static constexpr int PARTS = 1;
-  static __device__ __forceinline__ Acc mma(u32x4 a, u32x4 b, Acc c, int) {
-    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
-  }
+
+// The products of 32 bits of a large tile are formed of products of 16: a value is the sum
+// of three bfloat16, each the nearest to what the ones before it leave, and together they
+// hold all its 24 bits (a value under 2^-110 may lose its last ones).  Of the nine products
+// of two values' parts the six largest are summed; the others are 2^-22 of the whole
+// between them at the very most, and 2^-26 as a rule.  The matrix cores take sixteen times
+// as many 16-bit products as 32-bit ones, and forming the parts is what bounds it:
+// 16384 x 4096 x 1024 763 us, and 1010 with their 32-bit instructions.  Tiles of fewer rows
+// split a value for fewer products, and keep those (16 rows of 128256 x 2048: 181 us, split
+// 242).  What rounds to an infinity in 16 bits leaves a NaN.
+//
+// A lane's eight values are its chunks of either half of a tile: k 4g..4g+3 and 16 more on
+// both sides.
+struct Split {
+  bf16x8 part[3];
 };
+__device__ __forceinline__ Split split(u32x4 x, u32x4 y) {
+  typedef float f32x8 __attribute__((ext_vector_type(8)));
+  const u32x4 both[2] = {x, y};
+  f32x8 v = __builtin_bit_cast(f32x8, both);
+  Split s;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    s.part[i] = __builtin_convertvector(v, bf16x8);
+    if (i < 2) v -= __builtin_convertvector(s.part[i], f32x8);
+  }
+  return s;
+}
+
+template <int MI, int NI>
+__device__ __forceinline__ void multiply_split(f32x4 (&acc)[MI][NI], const u32x4 (&fa)[2][MI], const u32x4 (&fb)[2][NI]) {
+  constexpr int A[6] = {2, 0, 1, 1, 0, 0}, B[6] = {0, 2, 1, 0, 1, 0};  // the small ones first
+  Split a[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) a[i] = split(fa[0][i], fa[1][i]);
+#pragma unroll
+  for (int j = 0; j < NI; ++j) {
+    const Split b = split(fb[0][j], fb[1][j]);
+#pragma unroll
+    for (int p = 0; p < 6; ++p)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i].part[A[p]], b.part[B[p]], acc[i][j], 0, 0, 0);
+  }
+}
+
+// Whether a tile's products are split ones.
+template <typename T, class TL>
+constexpr bool kSplit = sizeof(T) == 4 && TL::SPLIT;
 
 // One side of a product: element (row, k) at p[row*stride + k], or p[k*stride + row] where
 // the loader is a transposing one.
@@ -141,6 +190,8 @@ struct Tile {
   static constexpr int THREADS = WM * WN * kWave;
   static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;  // 16x16 tiles of a wave
   static constexpr int LDS = (BM + BN) * kRowBytes;
+  static constexpr bool SPLIT = false;  // of 32 bits
+  static constexpr int WAVES = 1;  // of a SIMD, at least: what the registers are shared among
 };
 
 // Where a lane's values lie: value r of acc[i][j] is at m0 + m(i) + r, n0 + n(j).
@@ -342,7 +393,7 @@ __device__ __forceinline__ void interleave() {
 
 // ONCE: a is read once and does not stay in the last-level cache; its loads are marked so.
 template <typename T, class TL, bool ONCE, Load LA, Load LB, class Epilogue>
-__global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, Grid g, Epilogue e) {
+__global__ __launch_bounds__(TL::THREADS, TL::WAVES) void k_product_direct(Side a, Side b, Grid g, Epilogue e) {
   constexpr int STAGES = TL::STAGES;
   typedef Stream<T, TL::BM, TL::WM * TL::WN, LA, ONCE> SA;
   typedef Stream<T, TL::BN, TL::WM * TL::WN, LB, false> SB;
@@ -391,25 +442,33 @@ __global__ __launch_bounds__(TL::THREADS) void k_product_direct(Side a, Side b, 
 #pragma unroll
         for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[half][i], fb[half][j], acc[i][j], p);
   };
-  // Half a tile (64 bytes of k) is multiplied while the next half is read.  Before the first
-  // half of the next tile the workgroup meets: that tile has arrived (the STAGES - 2 behind
-  // it may be under way), and this one has been read by all, so its space takes a new one.
+  // Half a tile (64 bytes of k) is multiplied while the next half is read (split ones: a
+  // whole tile, and the other workgroup of the compute unit fills the wait).  Before the first half
+  // of the next tile the workgroup meets: that tile has arrived (the STAGES - 2 behind it may
+  // be under way), and this one has been read by all, so its space takes a new one.
   wait_and_meet<(STAGES - 1) * (SA::N + SB::N)>();
-  if (tiles > 0) read(0, lds);
+  if (!kSplit<T, TL> && tiles > 0) read(0, lds);
   int stage = 0;
   for (int i = 0; i < tiles; ++i) {
     char* const here = lds + stage * STAGE;
+    if constexpr (kSplit<T, TL>) read(0, here);
     read(1, here);
-    multiply(0);
-    interleave<TL, T, LA, LB, 0>();
+    if constexpr (!kSplit<T, TL>) {
+      multiply(0);
+      interleave<TL, T, LA, LB, 0>();
+    }
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     wait_and_meet<(STAGES - 2) * (SA::N + SB::N)>();
     sa.load(here, left, wave, lane);
     sb.load(here + SA::BYTES, left, wave, lane);
     left -= BK;
-    read(0, lds + stage * STAGE);  // of no use after the last tile
-    multiply(1);
-    interleave<TL, T, LA, LB, SA::N + SB::N>();
+    if constexpr (kSplit<T, TL>) {
+      multiply_split(acc, fa, fb);
+    } else {
+      read(0, lds + stage * STAGE);  // of no use after the last tile
+      multiply(1);
+      interleave<TL, T, LA, LB, SA::N + SB::N>();
+    }
   }
   wait_and_meet<0>();  // the epilogue may take the LDS
   e.template run<TL>(acc, place_of<TL>(q, a.rows, b.rows, wm, wn, lane, t), lds);
@@ -470,7 +529,7 @@ struct Carry : Layout<T, ROWS, WAVES, LOAD> {
 };
 
 template <typename T, class TL, Load LA, Load LB, class Epilogue>
-__global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g, Epilogue e) {
+__global__ __launch_bounds__(TL::THREADS, TL::WAVES) void k_product(Side a, Side b, Grid g, Epilogue e) {
   typedef Carry<T, TL::BM, TL::WM * TL::WN, LA> SA;
   typedef Carry<T, TL::BN, TL::WM * TL::WN, LB> SB;
   constexpr int BK = SA::BK;
@@ -509,20 +568,23 @@ __global__ __launch_bounds__(TL::THREADS) void k_product(Side a, Side b, Grid g,
     }
     const char* const tile = lds + stage * STAGE;
     stage ^= 1;
+    u32x4 fa[2][TL::MI], fb[2][TL::NI];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      u32x4 fa[TL::MI], fb[TL::NI];
 #pragma unroll
-      for (int i = 0; i < TL::MI; ++i) fa[i] = SA::fragment(tile, wm * TL::MI * 16 + i * 16, s, lane);
+      for (int i = 0; i < TL::MI; ++i) fa[s][i] = SA::fragment(tile, wm * TL::MI * 16 + i * 16, s, lane);
 #pragma unroll
-      for (int j = 0; j < TL::NI; ++j) fb[j] = SB::fragment(tile + SA::BYTES, wn * TL::NI * 16 + j * 16, s, lane);
+      for (int j = 0; j < TL::NI; ++j) fb[s][j] = SB::fragment(tile + SA::BYTES, wn * TL::NI * 16 + j * 16, s, lane);
+      if constexpr (!kSplit<T, TL>) {
 #pragma unroll
-      for (int p = 0; p < Mma<T>::PARTS; ++p)
+        for (int p = 0; p < Mma<T>::PARTS; ++p)
 #pragma unroll
-        for (int i = 0; i < TL::MI; ++i)
+          for (int i = 0; i < TL::MI; ++i)
 #pragma unroll
-          for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[i], fb[j], acc[i][j], p);
+            for (int j = 0; j < TL::NI; ++j) acc[i][j] = Mma<T>::mma(fa[s][i], fb[s][j], acc[i][j], p);
+      }
     }
+    if constexpr (kSplit<T, TL>) multiply_split(acc, fa, fb);
     if (left > BK) {  // into the space that all have read before they last met
       sa.store(lds + stage * STAGE, wave, lane);
       sb.store(lds + stage * STAGE + SA::BYTES, wave, lane);
@@ -563,7 +625,8 @@ __device__ __forceinline__ void store_rows(const Place<TL>& w, char* lds, T* out
       for (int r = 0; r < 4; ++r) v[r] = from_float<T>(value(i, j, r));
       const int at = (i * 16 + g * 4) * (int)sizeof(T);  // chunk c of row r lies at c ^ r
       __builtin_memcpy(__builtin_assume_aligned(
-                           mine + row * (CHUNKS * 16) + (((at >> 4) ^ (row & (CHUNKS - 1))) << 4) + (at & 15), 4 * sizeof(T)),
+                           mine + row * (CHUNKS * 16) + (((at >> 4) ^ (row & (CHUNKS - 1))) << 4) + (at & 15),
+                           4 * sizeof(T)),
                        v, sizeof v);
     }
     __builtin_amdgcn_wave_barrier();
@@ -991,6 +1054,20 @@ struct WideTile : Tile<128, 192, 2, 4> {  // two
 struct MediumTile : Tile<128, 128, 2, 4> {  // two
   static constexpr int STAGES = 2;
 };
+// Of 32 bits: a wave's values are split for itself, and four waves have fewer to split (us with
+// eight and four: 32000 x 1024 x 256 124 and 106, 16384 x 4096 x 1024 909 and 763).
+struct Medium32Tile : Tile<128, 128, 2, 2> {
+  static constexpr bool SPLIT = true;
+  static constexpr int STAGES = 2, WAVES = 2;
+};
+template <typename T>
+struct MediumOf {
+  typedef MediumTile Tile;
+};
+template <>
+struct MediumOf<float> {
+  typedef Medium32Tile Tile;
+};
 struct LowTile : Tile<128, 64, 4, 2> {
   static constexpr int STAGES = 3;
 };
@@ -1056,9 +1133,8 @@ struct Cut {
 };
 // What a round of workgroups of a shape takes: us per tile of 128 bytes of k for a
 // workgroup alone on its compute unit and for as many as the chip holds (slots, on 256
-// compute units), and us for its start and end.  32 bits are bound by the matrix cores
-// whatever the tile (the large one spilled registers: 146 against 143 us for
-// 32000 x 1024 x 256).
+// compute units), and us for its start and end.  32 bits have no larger tiles: with split
+// products 128 x 192 took 136 us and 256 x 256 239 for 32000 x 1024 x 256, 128 x 128 106.
 struct Pace {
   Shape shape;
   double alone, full;
@@ -1070,13 +1146,13 @@ constexpr Pace kPaces[] = {{Shape::Large, 1.27, 1.45, 256, 7.0},
                            {Shape::Medium, 0.57, 0.92, 512, 2.0},
                            {Shape::Low, 0.35, 0.62, 512, 2.0},
                            {Shape::Small, 0.25, 0.60, 768, 2.0}};
-constexpr Pace kPaces32[] = {{Shape::Medium, 1.95, 3.9, 512, 4.0},
+constexpr Pace kPaces32[] = {{Shape::Medium, 1.85, 3.0, 512, 3.0},
                              {Shape::Low, 0.98, 2.1, 512, 2.5},
                              {Shape::Small, 0.49, 1.55, 768, 2.0}};
 // Operands through registers: a workgroup alone waits for its loads, and two fill the gaps
 // (1550 x 103477 x 2127 in 8 bits 38 us a round, 2048 x 50257 x 768 bf16 19).
 constexpr Pace kPacesAny[] = {{Shape::Medium, 1.5, 1.6, 512, 2.0}, {Shape::Small, 0.9, 1.2, 768, 2.0}};
-constexpr Pace kPacesAny32[] = {{Shape::Medium, 2.6, 4.2, 512, 4.0}, {Shape::Small, 1.1, 1.9, 768, 2.0}};
+constexpr Pace kPacesAny32[] = {{Shape::Medium, 2.4, 3.5, 512, 3.0}, {Shape::Small, 1.1, 1.9, 768, 2.0}};
 double expected_us(const Pace& p, int64_t groups, int64_t tiles_k) {
   const int64_t rounds = (groups - 1) / p.slots, last = groups - rounds * p.slots;
   return rounds * (tiles_k * p.full + p.start) + tiles_k * (last <= 256 ? p.alone : p.full) + p.start;
@@ -1137,7 +1213,7 @@ void launch_product(Way way, const Side& a, const Side& b, int64_t k, int parts,
     } else if (s == Shape::Small) {
       if constexpr (LA == Load::Rows) launch_any<T, SmallTile, LA, LB>(a, b, g, groups, e, st);
     } else if constexpr (LB == Load::Rows) {
-      launch_any<T, MediumTile, LA, LB>(a, b, g, groups, e, st);
+      launch_any<T, typename MediumOf<T>::Tile, LA, LB>(a, b, g, groups, e, st);
     }
     return;
   }
@@ -1148,7 +1224,7 @@ void launch_product(Way way, const Side& a, const Side& b, int64_t k, int parts,
     case Shape::Wide:
       if constexpr (sizeof(T) < 4) launch_direct<T, WideTile, LA, LB>(a, b, g, groups, e, st);
       break;
-    case Shape::Medium: launch_direct<T, MediumTile, LA, LB>(a, b, g, groups, e, st); break;
+    case Shape::Medium: launch_direct<T, typename MediumOf<T>::Tile, LA, LB>(a, b, g, groups, e, st); break;
     case Shape::Low:  // row-major operands (cut_of)
       if constexpr (LA == Load::Rows) launch_few<T, LowTile, LA, LB>(a, b, g, groups, e, st);
       break;
